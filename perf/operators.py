@@ -4,8 +4,10 @@ Four operators, each one pass as a training or serving program makes it:
 
   dropout   y = keep(x) * scale [+ add], the mask from a counter-based generator and never stored.  The backward pass is the
             same call on the gradient.
-  quantize  a matrix into 8-bit floating point with one scale for each block of 128 entries of a row (activations, gradients)
-            or each tile of 128 x 128 (weights), and the same of its transpose, which the backward products read
+  quantize  a matrix into 8-bit floating point with one scale, a power of two, for each block of 128 entries of a row
+            (activations, gradients) or each tile of 128 x 128 (weights), and the same of its transpose, which the backward
+            products read.  A scale is stored as its exponent plus 127; values [rows][columns up to a multiple of 128],
+            scales [blocks of columns][rows up to a multiple of 128], a tile's rows all with the tile's scale
   product   y[m,n] = sum over blocks of a_scale * b_scale * (sum over the block of a[m,k] * b[n,k]): the forward product of a
             layer, and on other operands its two backward products
   head      softmax cross entropy of a linear last layer over a large vocabulary: loss and log-sum of every token, and, in a
@@ -21,9 +23,8 @@ import torch
 own = False
 
 BLOCK = 128
-FORMATS = {"e4m3": (torch.float8_e4m3fn, 448.0), "e5m2": (torch.float8_e5m2, 57344.0)}
+FORMATS = {"e4m3": (torch.float8_e4m3fn, 8), "e5m2": (torch.float8_e5m2, 15)}      # largest value 1.75 * 2 ** that
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
-LEAST = 2.0 ** -100        # smallest magnitude that a block's scale is made for
 
 
 def _dropout(n, p, type, add):
@@ -131,12 +132,11 @@ def prepare(case, seed):
         rows, cols = c["rows"], c["cols"]
         x = torch.randn((rows, cols), device="cuda", generator=gen) * 0.02 if c["tiles"] else _activations((rows, cols), gen)
         s["x"] = x.to(TYPES[c["type"]])
-        across = 1 if not c["tiles"] else BLOCK
         s["q"] = torch.empty((rows, _blocks(cols) * BLOCK), dtype=torch.uint8, device="cuda")
-        s["scale"] = torch.empty((_blocks(cols), -(-rows // across)), device="cuda")
+        s["scale"] = torch.empty((_blocks(cols), _blocks(rows) * BLOCK), dtype=torch.uint8, device="cuda")
         if c["both"]:
             s["q_t"] = torch.empty((cols, _blocks(rows) * BLOCK), dtype=torch.uint8, device="cuda")
-            s["scale_t"] = torch.empty((_blocks(rows), -(-cols // across)), device="cuda")
+            s["scale_t"] = torch.empty((_blocks(rows), _blocks(cols) * BLOCK), dtype=torch.uint8, device="cuda")
     elif c["kind"] == "product":
         M, N, K = c["M"], c["N"], c["K"]
         s["a"], s["a_scale"] = _plain_quantize(_activations((M, K), gen), c["format"], False)
@@ -201,11 +201,9 @@ def _run_product(s):
     if own:
         import paper_2501_09849_amd as cdl
         fmt = cdl.E4M3 if c["format"] == "e4m3" else cdl.E5M2
-        cdl.cdl_block8_gemm(s["a"], s["a_scale"], s["b"], s["b_scale"], c["M"], c["N"], c["K"], s["y"], s["ws"], a_format=fmt, b_tiles=c["tiles"])
+        cdl.cdl_block8_gemm(s["a"], s["a_scale"], s["b"], s["b_scale"], c["M"], c["N"], c["K"], s["y"], s["ws"], a_format=fmt)
         return s["y"]
-    a = _plain_values(s["a"], s["a_scale"], False)
-    b = _plain_values(s["b"], s["b_scale"], c["tiles"])
-    return (a @ b.t()).to(TYPES[c["out"]])
+    return (_plain_values(s["a"], s["a_scale"]) @ _plain_values(s["b"], s["b_scale"]).t()).to(TYPES[c["out"]])
 
 
 def _run_head(s):
@@ -252,21 +250,26 @@ def _plain_halves(n, key, counter):
 
 
 def _plain_quantize(x, fmt, tiles):
-    """(values [rows, whole blocks of columns], scales [blocks of columns, rows or tiles of rows]) of x in 32 bits."""
-    kind, most = FORMATS[fmt]
+    """(values, scales) of x in 32 bits: the smallest scale under which the largest magnitude is no larger than the format's, 2 ** -126 at least."""
+    kind, top = FORMATS[fmt]
     rows, cols = x.shape
-    r = BLOCK if tiles else 1
-    p = torch.nn.functional.pad(x, (0, -cols % BLOCK, 0, -rows % r))
-    p = p.reshape(p.shape[0] // r, r, -1, BLOCK)
-    largest = p.abs().amax(dim=(1, 3)).clamp(min=LEAST)
-    q = (p * (most / largest)[:, None, :, None]).to(kind)
-    return q.reshape(-1, _blocks(cols) * BLOCK)[:rows].contiguous(), (largest / most).t().contiguous()
+    p = torch.nn.functional.pad(x, (0, -cols % BLOCK, 0, -rows % BLOCK)).reshape(_blocks(rows), BLOCK, _blocks(cols), BLOCK)
+    largest = p.abs().amax(dim=(1, 3) if tiles else 3, keepdim=True)
+    fraction, exponent = torch.frexp(largest)      # largest = fraction * 2 ** exponent, fraction in [0.5, 1)
+    exponent = torch.where(largest > 0, exponent - 1 - top + (fraction > 0.875).int(), -126).clamp(min=-126)
+    q = (p * _power(-exponent)).to(kind)
+    scale = (exponent + 127).to(torch.uint8).expand(-1, BLOCK, -1, -1).reshape(-1, _blocks(cols)).t().contiguous()
+    return q.reshape(-1, _blocks(cols) * BLOCK)[:rows].contiguous(), scale
 
 
-def _plain_values(q, scale, tiles):
-    s = scale.t().repeat_interleave(BLOCK, dim=1)
-    s = s.repeat_interleave(BLOCK, dim=0)[: q.shape[0]] if tiles else s
-    return q.float() * s
+def _plain_values(q, scale):
+    by = _power(scale[:, : q.shape[0]].int() - 127)
+    return q.float() * by.t().repeat_interleave(BLOCK, dim=1)
+
+
+def _power(exponent):
+    """2 ** exponent, exactly, for exponents from -126 to 127."""
+    return ((exponent + 127) << 23).int().view(torch.float32)
 
 
 # ---- what the work cannot do without ----------------------------------------------------------------------------------
@@ -281,8 +284,7 @@ def work(case):
         return {"bytes": n * (size[c["type"]] + (2 if c["both"] else 1)), "flops": 3 * n}
     if c["kind"] == "product":
         M, N, K = c["M"], c["N"], c["K"]
-        kb = _blocks(K)
-        scales = 4 * kb * (M + (_blocks(N) if c["tiles"] else N))
+        scales = _blocks(K) * (M + (_blocks(N) if c["tiles"] else N))
         return {"bytes": M * K + N * K + scales + M * N * size[c["out"]], "flops": 2 * M * N * K}
     T, V, D = c["T"], c["V"], c["D"]
     ends = (T * D + V * D) * size[c["type"]]
@@ -302,13 +304,11 @@ def exact(case, seed):
         return out + [*_exact_quantize(x.t(), c)] if c["both"] else out
     if c["kind"] == "product":
         y = torch.zeros((c["M"], c["N"]), dtype=torch.float64, device="cuda")
-        spread = BLOCK if c["tiles"] else 1
-        row = torch.arange(c["N"], device="cuda") // spread
         step = BLOCK * max(1, _blocks(c["K"]) // 16)
         for k in range(0, c["K"], step):      # a stretch of blocks at a time
             block = torch.arange(k, min(k + step, s["a"].shape[1]), device="cuda") // BLOCK
-            a = s["a"][:, k:k + step].double() * s["a_scale"].double()[block].t()
-            b = s["b"][:, k:k + step].double() * s["b_scale"].double()[block][:, row].t()
+            a = torch.ldexp(s["a"][:, k:k + step].double(), s["a_scale"].t()[: c["M"], block].int() - 127)
+            b = torch.ldexp(s["b"][:, k:k + step].double(), s["b_scale"].t()[: c["N"], block].int() - 127)
             y += a @ b.t()
         return y
     return _exact_head(c, s)
@@ -340,14 +340,17 @@ def _exact_dropout(c, s):
 
 
 def _exact_quantize(x, c):
-    kind, most = FORMATS[c["format"]]
+    kind, top = FORMATS[c["format"]]
     rows, cols = x.shape
-    r = BLOCK if c["tiles"] else 1
-    full = torch.zeros((-(-rows // r) * r, _blocks(cols) * BLOCK), dtype=torch.float64, device="cuda")
+    full = torch.zeros((_blocks(rows) * BLOCK, _blocks(cols) * BLOCK), dtype=torch.float64, device="cuda")
     full[:rows, :cols] = x
-    scale = full.abs().unflatten(0, (-1, r)).unflatten(2, (-1, BLOCK)).amax(dim=3).amax(dim=1).clamp(min=LEAST) / most
-    full /= scale.repeat_interleave(r, dim=0).repeat_interleave(BLOCK, dim=1)
-    return full[:rows].to(kind).double(), scale.t()
+    size = full.abs().unflatten(1, (-1, BLOCK)).amax(dim=2)
+    if c["tiles"]:
+        size = size.unflatten(0, (-1, BLOCK)).amax(dim=1).repeat_interleave(BLOCK, dim=0)
+    power = torch.ceil(torch.log2(size / (1.75 * 2.0 ** top))).clamp(min=-126)
+    power += (size > 1.75 * torch.exp2(power + top)).double() - (size <= 1.75 * torch.exp2(power + top - 1)).double() * (power > -126)      # (where the logarithm rounds across a whole number)
+    full /= torch.exp2(power).repeat_interleave(BLOCK, dim=1)
+    return full[:rows].to(kind).double(), (power + 127).t().to(torch.uint8)
 
 
 def _exact_head(c, s):

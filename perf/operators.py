@@ -250,13 +250,13 @@ def _plain_halves(n, key, counter):
 
 
 def _plain_quantize(x, fmt, tiles):
-    """(values, scales) of x in 32 bits: the smallest scale under which the largest magnitude is no larger than the format's, 2 ** -126 at least."""
+    """(values, scales) of x in 32 bits: the smallest scale under which the largest magnitude is no larger than the format's, 2 ** -100 at least."""
     kind, top = FORMATS[fmt]
     rows, cols = x.shape
     p = torch.nn.functional.pad(x, (0, -cols % BLOCK, 0, -rows % BLOCK)).reshape(_blocks(rows), BLOCK, _blocks(cols), BLOCK)
     largest = p.abs().amax(dim=(1, 3) if tiles else 3, keepdim=True)
     fraction, exponent = torch.frexp(largest)      # largest = fraction * 2 ** exponent, fraction in [0.5, 1)
-    exponent = torch.where(largest > 0, exponent - 1 - top + (fraction > 0.875).int(), -126).clamp(min=-126)
+    exponent = torch.where(largest > 0, exponent - 1 - top + (fraction > 0.875).int(), -100).clamp(min=-100)
     q = (p * _power(-exponent)).to(kind)
     scale = (exponent + 127).to(torch.uint8).expand(-1, BLOCK, -1, -1).reshape(-1, _blocks(cols)).t().contiguous()
     return q.reshape(-1, _blocks(cols) * BLOCK)[:rows].contiguous(), scale
@@ -347,8 +347,8 @@ def _exact_quantize(x, c):
     size = full.abs().unflatten(1, (-1, BLOCK)).amax(dim=2)
     if c["tiles"]:
         size = size.unflatten(0, (-1, BLOCK)).amax(dim=1).repeat_interleave(BLOCK, dim=0)
-    power = torch.ceil(torch.log2(size / (1.75 * 2.0 ** top))).clamp(min=-126)
-    power += (size > 1.75 * torch.exp2(power + top)).double() - (size <= 1.75 * torch.exp2(power + top - 1)).double() * (power > -126)      # (where the logarithm rounds across a whole number)
+    power = torch.ceil(torch.log2(size / (1.75 * 2.0 ** top))).clamp(min=-100)
+    power += (size > 1.75 * torch.exp2(power + top)).double() - (size <= 1.75 * torch.exp2(power + top - 1)).double() * (power > -100)      # (where the logarithm rounds across a whole number)
     full /= torch.exp2(power).repeat_interleave(BLOCK, dim=1)
     return full[:rows].to(kind).double(), (power + 127).t().to(torch.uint8)
 

@@ -13,7 +13,8 @@
  * alphabet), cdl_qgemm_bwd_quantize_bwd (the last two steps in one call), cdl_qgemm_fwd_quantize (the second and
  * third), cdl_qconv_fwd / cdl_qconv_bwd_weights / cdl_qconv_bwd_activations (a convolutional layer on [B,H,W,C]
  * activations), cdl_quantize_fwd_static (no workspace); next to the path: cdl_marginal_entropy, cdl_entropy_bwd,
- * cdl_quantize_draw, cdl_huffman_bits.
+ * cdl_quantize_draw, cdl_huffman_bits; layers in 8-bit floating point, their loss and dropout: cdl_block8_quantize, cdl_block8_gemm,
+ * cdl_head_loss_fwd / cdl_head_loss_bwd, cdl_dropout.
  *
  * Conventions for every entry point
  *   - All tensor and scalar-output pointers are DEVICE pointers owned by the caller; tensors are
@@ -382,6 +383,88 @@ int cdl_qgemm_bwd_quantize_bwd(const float *g, const int8_t *a_idx, const int8_t
                                float *d_theta_a, float *d_delta_a, float *d_alpha_a, float *d_b_hat,
                                const float *theta_b, const cdl_qparams *p_b, float *d_theta_b, float *d_delta_b, float *d_alpha_b,
                                void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * ---- A network in eight bits: what stands next to the quantized layer step ----------------------------------------
+ *
+ * Tensors of these entry points are fp32 or bf16, as `type` says; all other conventions are those above.
+ */
+enum { CDL_F32 = 0, CDL_BF16 = 1 };
+
+/* Formats of 8-bit floating point: 4 exponent bits (largest value 448), 5 exponent bits (largest value 57344). */
+enum { CDL_E4M3 = 0, CDL_E5M2 = 1 };
+
+/* n rounded up to a whole number of blocks of 128 (0 for a negative n): the pitch of the rows below. */
+int64_t cdl_block8_pitch(int32_t n);
+
+/*
+ * A matrix x[rows, cols] in 8-bit floating point with a scale for each block, an alternative to level indices where a
+ * layer stays at eight bits (the first and the last one, Sec. V-B): one for every 128 entries of a row, or, with `tiles`
+ * not 0, one for every tile of 128 x 128 entries.  A block's scale s is the smallest power of two, 2^-100 at least, with
+ * max|x| <= s * (largest value of the format), and an entry is stored as x / s rounded to the nearest value, ties to even.
+ *   q       [rows][pitch(cols)]               the bytes, zeros beyond cols
+ *   scale   [blocks of cols][pitch(rows)]     log2(s) + 127, a byte for every row and block (with tiles, the 128 rows of a
+ *                                             tile hold the same byte); 27 beyond rows, unless a tile reaches there
+ *   q_t     [cols][pitch(rows)], scale_t [blocks of rows][pitch(cols)]   the same of the transpose of x, whose blocks run
+ *           down the columns of x: the operands of the backward products.  With tiles the values are those of q.
+ * pitch(n) = cdl_block8_pitch(n).  Either pair (q, scale) or (q_t, scale_t) may be NULL, not
+ * both.  A block with an entry that is not finite gets scale 255 and its products come out NaN.  x 16-byte aligned, as are the outputs.
+ */
+int cdl_block8_quantize(const void *x, int32_t type, int32_t rows, int32_t cols, int32_t tiles, int32_t format,
+                        uint8_t *q, uint8_t *scale, uint8_t *q_t, uint8_t *scale_t, void *hip_stream);
+
+/*
+ * Product of two such matrices over their contiguous dimension, which is the one their blocks run along:
+ *   y[m,n] = sum_kb a_scale[kb,m] * b_scale[kb,n] * sum_{k in block kb} a[m,k] * b[n,k]     (y[M,N], fp32 or bf16 by y_type)
+ * a [M][pitch(K)] with a_scale [blocks of K][pitch(M)], b [N][pitch(K)] with b_scale [blocks of K][pitch(N)], as
+ * cdl_block8_quantize writes them (bytes beyond K have to be zero; scale bytes 1 .. 254).  Into fp32: products are exact and sums
+ * fp32 (an entry below 2^-126 in value counts as 0; the quantizer makes none).  Into bf16: the matrix instructions for 8-bit operands, at twice the rate, which of every product keep what lies above 2^-14 of the largest of the 16
+ * that they add up first (1.5e-5 of the result over random operands), sums in fp32, one rounding.  With x -> (q, scale) of the activations, w -> tiles of the weights and g -> the gradient of the output,
+ *   forward y = x . w^T          a = x,     b = w
+ *   d_x = g . w                  a = g,     b = w's (q_t, scale_t)
+ *   d_w = g^T . x                a = g's (q_t, scale_t),  b = x's (q_t, scale_t)
+ * Same inputs, same bits.  K == 0 gives zeros.  CDL_ERR_RANGE for K > 2^23, M or N > 2^30 or M * N > 2^44.  Scratch:
+ * cdl_block8_gemm_workspace_bytes (0 where the contraction is not split), 256-byte aligned.
+ */
+size_t cdl_block8_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K);
+int cdl_block8_gemm(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale,
+                    int32_t M, int32_t N, int32_t K, int32_t a_format, int32_t b_format, void *y, int32_t y_type,
+                    void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Softmax cross entropy of a linear last layer (the loss L of the objective, eq. obj, for a network whose classes are a
+ * vocabulary): h[T,D] hidden states, w[V,D] the layer's weights, both of `type`, z = h . w^T never in memory as a whole.
+ *   lse[t]  = log sum_v exp(z[t,v])                                  (fp32[T], required)
+ *   loss[t] = lse[t] - z[t, target[t]]                               (fp32[T], nullable)
+ * target: int64[T].  A token whose target lies outside [0, V) is padding: loss 0; its lse is formed.  Nothing that a
+ * padding token holds reaches any other token, unless it is not finite (0 times infinity in d_w).
+ *
+ * Backward, with the lse of the forward call: for d_loss, d_lse the gradients of those outputs (fp32[T]; NULL: d_loss 1, d_lse 0),
+ *   g[t,v] = (d_loss[t] + d_lse[t]) * exp(z[t,v] - lse[t]) - d_loss[t] * [v = target[t]],      d_loss[t] taken as 0 for padding,
+ *   d_h[t,:] = sum_v g[t,v] w[v,:]   (type, [T,D], nullable),    d_w[v,:] = sum_t g[t,v] h[t,:]   (type, [V,D], nullable)
+ * z is formed again, a piece of the vocabulary at a time; for bf16, g (divided by the largest |d_loss| + |d_lse|) is rounded to bf16
+ * before its two products, all sums are fp32.  For fp32 every operand is used as three bf16 parts, which hold it whole, and the six
+ * products of parts that matter in fp32 are summed.  At least one output.  Same inputs, same bits.
+ * `train` != 0: scratch for the backward call too (the forward call takes either).  256-byte aligned, as for all calls.
+ * V >= 1 unless T == 0 (CDL_ERR_PARAM).  D == 0: z = 0.  CDL_ERR_RANGE for D > 2^20, T > 2^22, V > 2^30 or T * V > 2^44.
+ */
+size_t cdl_head_loss_workspace_bytes(int32_t T, int32_t V, int32_t D, int32_t type, int32_t train);
+int cdl_head_loss_fwd(const void *h, const void *w, int32_t type, const int64_t *target, int32_t T, int32_t V, int32_t D,
+                      float *loss, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+int cdl_head_loss_bwd(const void *h, const void *w, int32_t type, const int64_t *target, const float *lse,
+                      const float *d_loss, const float *d_lse, int32_t T, int32_t V, int32_t D,
+                      void *d_h, void *d_w, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Dropout whose mask is computed, never stored: y[e] = (kept(e) ? x[e] / (1 - r) : 0) + add[e], r being p in [0, 1]
+ * rounded to a multiple of 2^-16 and add nullable (0; a residual, say).  kept(e) is [16 random bits >= 65536 r]; the bits of entries 8 i .. 8 i + 7 are the
+ * low and high halves of the four words that the Philox 4x32 generator (Salmon et al., SC 2011; ten rounds) gives for the key `seed`
+ * and the counter `counter` + i (each as 64 bits, low word first; the upper two counter words zero).  The backward pass is the same call on the gradient.  Calls with
+ * the same seed are independent where their ranges of counters, (n + 7) / 8 long, do not overlap.  r = 1 drops everything.
+ * y may be x or add.  One rounding, from fp32.  x, add, y: `type`, 16-byte aligned.
+ */
+int cdl_dropout(const void *x, const void *add, int32_t type, int64_t n, float p, uint64_t seed, uint64_t counter,
+                void *y, void *hip_stream);
 
 /*
  * Optional per-kernel timing (a measurement aid, not part of the method).  While enabled, every

@@ -11,5 +11,7 @@ from .binding import (  # noqa: F401
     qconv_fwd_workspace_bytes, cdl_qconv_fwd, cdl_qgemm_fwd_quantize, qconv_bwd_weights_workspace_bytes, cdl_qconv_bwd_weights,
     qconv_bwd_activations_workspace_bytes, cdl_qconv_bwd_activations,
     cdl_quantize_draw, cdl_entropy_bwd, huffman_workspace_bytes, cdl_huffman_bits,
+    F32, BF16, E4M3, E5M2, block8_pitch, cdl_block8_quantize, block8_gemm_workspace_bytes, cdl_block8_gemm,
+    head_loss_workspace_bytes, cdl_head_loss_fwd, cdl_head_loss_bwd, cdl_dropout,
     cdl_profile_enable, cdl_profile_collect, cdl_profile_only, cdl_probe_mfma_int8, EXPORTS,
 )

@@ -18,7 +18,8 @@ _CALLS = None      # the native module, once the library is loaded
 
 _MARSHALLED = ("cdl_quantize_fwd", "cdl_quantize_bwd", "cdl_marginal_entropy", "cdl_quantize_draw", "cdl_entropy_bwd", "cdl_huffman_bits",
                "cdl_qgemm_fwd_offset", "cdl_qgemm_bwd_offset", "cdl_qgemm_fwd_quantize", "cdl_qconv_fwd", "cdl_qconv_bwd_weights",
-               "cdl_qconv_bwd_activations", "cdl_qgemm_bwd_quantize_bwd")
+               "cdl_qconv_bwd_activations", "cdl_qgemm_bwd_quantize_bwd", "cdl_block8_quantize", "cdl_block8_gemm", "cdl_head_loss_fwd",
+               "cdl_head_loss_bwd", "cdl_dropout")
 
 EXPORTS = (
     "cdl_quantize_workspace_bytes", "cdl_qgemm_fwd_workspace_bytes", "cdl_qgemm_bwd_workspace_bytes",
@@ -28,9 +29,14 @@ EXPORTS = (
     "cdl_qconv_bwd_activations_workspace_bytes", "cdl_qconv_bwd_activations",
     "cdl_quantize_fwd", "cdl_quantize_fwd_static", "cdl_static_scratch_bytes", "cdl_quantize_bwd", "cdl_marginal_entropy", "cdl_qgemm_fwd", "cdl_qgemm_bwd",
     "cdl_quantize_draw", "cdl_entropy_bwd", "cdl_huffman_workspace_bytes", "cdl_huffman_bits",
+    "cdl_block8_pitch", "cdl_block8_quantize", "cdl_block8_gemm_workspace_bytes", "cdl_block8_gemm",
+    "cdl_head_loss_workspace_bytes", "cdl_head_loss_fwd", "cdl_head_loss_bwd", "cdl_dropout",
     "cdl_profile_enable", "cdl_profile_collect", "cdl_profile_only", "cdl_probe_mfma_int8",
     "cdl_status_string", "cdl_last_hip_error", "cdl_version",
 )
+
+F32, BF16 = 0, 1          # element types
+E4M3, E5M2 = 0, 1         # formats of 8-bit floating point
 
 
 class CdlError(RuntimeError):
@@ -143,6 +149,23 @@ def load():
         L.cdl_qgemm_bwd_quantize_bwd.argtypes = [vp, vp, vp, i32, i32, i32, vp, qp, f32, i32, vp, vp, vp, vp, vp, qp, vp, vp, vp, vp, sz, vp]
         L.cdl_qgemm_bwd_offset.restype = ctypes.c_int
         L.cdl_qgemm_bwd_offset.argtypes = [vp, vp, vp, i32, i32, i32, f32, f32, i32, i32, vp, vp, vp, sz, vp]
+        u64 = ctypes.c_uint64
+        L.cdl_block8_pitch.restype = i64
+        L.cdl_block8_pitch.argtypes = [i32]
+        L.cdl_block8_quantize.restype = ctypes.c_int
+        L.cdl_block8_quantize.argtypes = [vp] + [i32] * 5 + [vp] * 5
+        L.cdl_block8_gemm_workspace_bytes.restype = sz
+        L.cdl_block8_gemm_workspace_bytes.argtypes = [i32, i32, i32]
+        L.cdl_block8_gemm.restype = ctypes.c_int
+        L.cdl_block8_gemm.argtypes = [vp] * 4 + [i32] * 5 + [vp, i32, vp, sz, vp]
+        L.cdl_head_loss_workspace_bytes.restype = sz
+        L.cdl_head_loss_workspace_bytes.argtypes = [i32] * 5
+        L.cdl_head_loss_fwd.restype = ctypes.c_int
+        L.cdl_head_loss_fwd.argtypes = [vp, vp, i32, vp, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.cdl_head_loss_bwd.restype = ctypes.c_int
+        L.cdl_head_loss_bwd.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.cdl_dropout.restype = ctypes.c_int
+        L.cdl_dropout.argtypes = [vp, vp, i32, i64, f32, u64, u64, vp, vp]
         L.cdl_profile_enable.restype = ctypes.c_int
         L.cdl_profile_enable.argtypes = [ctypes.c_int]
         L.cdl_profile_only.restype = ctypes.c_int
@@ -328,6 +351,79 @@ def cdl_qconv_fwd(x_idx, w_idx, B, H, W, C, N, R, S, stride, pad, delta_x, delta
                   x_offset=0):
     _check((_CALLS or _calls()).cdl_qconv_fwd(x_idx, w_idx, B, H, W, C, N, R, S, stride, pad, delta_x, delta_w, x_offset, acc, y, ws, stream),
            "cdl_qconv_fwd")
+
+
+_TYPES = {"torch.float32": F32, "torch.bfloat16": BF16}
+_TYPE_OF = {}             # the same by dtype, filled as they are met
+
+
+def _type_of(t, given=None) -> int:
+    """F32 or BF16: what is given, or the tensor's own (an address has none)."""
+    if given is not None:
+        return given
+    dtype = getattr(t, "dtype", None)
+    kind = _TYPE_OF.get(dtype)
+    if kind is None:
+        kind = _TYPES.get(str(dtype))
+        if kind is None:
+            raise TypeError("a float32 or bfloat16 tensor, or the type of an address, is needed: got %s" % (dtype,))
+        _TYPE_OF[dtype] = kind
+    return kind
+
+
+def _same_type(what, first, *others) -> None:
+    """Tensors of another type than the first would be read or written beyond their ends.  Addresses and None have none."""
+    like = getattr(first, "dtype", None)
+    if like is not None:
+        for t in others:
+            dtype = getattr(t, "dtype", like)
+            if dtype is not like:
+                raise TypeError("%s: %s tensors are needed, got %s" % (what, like, dtype))
+
+
+def block8_pitch(n: int) -> int:
+    return int(load().cdl_block8_pitch(n))
+
+
+def cdl_block8_quantize(x, rows, cols, q=None, scale=None, q_t=None, scale_t=None, tiles=False, format=E4M3, stream=None, type=None):
+    _check((_CALLS or _calls()).cdl_block8_quantize(x, _type_of(x, type), rows, cols, 1 if tiles else 0, format, q, scale, q_t, scale_t, stream),
+           "cdl_block8_quantize")
+
+
+def block8_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load().cdl_block8_gemm_workspace_bytes(M, N, K))
+
+
+def cdl_block8_gemm(a, a_scale, b, b_scale, M, N, K, y, ws=None, stream=None, a_format=E4M3, b_format=E4M3, y_type=None):
+    _check((_CALLS or _calls()).cdl_block8_gemm(a, a_scale, b, b_scale, M, N, K, a_format, b_format, y, _type_of(y, y_type), ws, stream),
+           "cdl_block8_gemm")
+
+
+def head_loss_workspace_bytes(T: int, V: int, D: int, type: int, train: bool = False) -> int:
+    return int(load().cdl_head_loss_workspace_bytes(T, V, D, type, 1 if train else 0))
+
+
+def _index_type(target) -> None:
+    if str(getattr(target, "dtype", "torch.int64")) != "torch.int64":
+        raise TypeError("targets are int64: got %s" % (target.dtype,))
+
+
+def cdl_head_loss_fwd(h, w, target, T, V, D, loss, lse, ws=None, stream=None, type=None):
+    _same_type("cdl_head_loss_fwd", h, w)
+    _index_type(target)
+    _check((_CALLS or _calls()).cdl_head_loss_fwd(h, w, _type_of(h, type), target, T, V, D, loss, lse, ws, stream), "cdl_head_loss_fwd")
+
+
+def cdl_head_loss_bwd(h, w, target, lse, T, V, D, d_h=None, d_w=None, ws=None, d_loss=None, d_lse=None, stream=None, type=None):
+    _same_type("cdl_head_loss_bwd", h, w, d_h, d_w)
+    _index_type(target)
+    _check((_CALLS or _calls()).cdl_head_loss_bwd(h, w, _type_of(h, type), target, lse, d_loss, d_lse, T, V, D, d_h, d_w, ws, stream),
+           "cdl_head_loss_bwd")
+
+
+def cdl_dropout(x, n, p, seed, counter, y, add=None, stream=None, type=None):
+    _same_type("cdl_dropout", x, add, y)
+    _check((_CALLS or _calls()).cdl_dropout(x, add, _type_of(x, type), n, p, seed, counter, y, stream), "cdl_dropout")
 
 
 def cdl_probe_mfma_int8(iters: int, random_operands: bool, blocks: int, sink, stream=None) -> float:

@@ -484,6 +484,101 @@ int cdl_qgemm_bwd(const float *g, const int8_t *a_idx, const int8_t *b_idx,
     return cdl_qgemm_bwd_offset(g, a_idx, b_idx, M, N, K, delta_a, delta_b, 0, 0, d_a_hat, d_b_hat, ws, ws_bytes, hip_stream);
 }
 
+// ---- layers in 8-bit floating point, the loss, dropout ---------------------------------------
+
+namespace {
+bool type_ok(int32_t t) { return t == CDL_F32 || t == CDL_BF16; }
+bool format_ok(int32_t f) { return f == CDL_E4M3 || f == CDL_E5M2; }
+}
+
+int64_t cdl_block8_pitch(int32_t n) { return block8_pitch(n); }
+
+int cdl_block8_quantize(const void *x, int32_t type, int32_t rows, int32_t cols, int32_t tiles, int32_t format,
+                        uint8_t *q, uint8_t *scale, uint8_t *q_t, uint8_t *scale_t, void *hip_stream)
+{
+    if (rows < 0 || cols < 0 || !type_ok(type) || !format_ok(format)) return CDL_ERR_PARAM;
+    if (!q != !scale || !q_t != !scale_t || (!q && !q_t)) return CDL_ERR_NULL;
+    if (rows > 0 && cols > 0 && !x) return CDL_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(q, 16) || !aligned(scale, 16) || !aligned(q_t, 16) || !aligned(scale_t, 16)) return CDL_ERR_ALIGN;
+    return launch_block8_quantize(x, type, rows, cols, tiles, format, q, scale, q_t, scale_t, (hipStream_t)hip_stream);
+}
+
+size_t cdl_block8_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K)
+{
+    if (M < 0 || N < 0 || K < 0) return 0;
+    return block8_gemm_workspace_bytes(M, N, K);
+}
+
+int cdl_block8_gemm(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale,
+                    int32_t M, int32_t N, int32_t K, int32_t a_format, int32_t b_format, void *y, int32_t y_type,
+                    void *ws, size_t ws_bytes, void *hip_stream)
+{
+    if (M < 0 || N < 0 || K < 0 || !format_ok(a_format) || !format_ok(b_format) || !type_ok(y_type)) return CDL_ERR_PARAM;
+    // 256 rows of an operand within 32-bit offsets; entries and tiles of the result counted in 32 bits
+    if (K > 1 << 23 || M > 1 << 30 || N > 1 << 30 || (int64_t)M * N > (int64_t)1 << 44) return CDL_ERR_RANGE;
+    if (M == 0 || N == 0) return CDL_OK;
+    if (!y || (K > 0 && (!a || !a_scale || !b || !b_scale))) return CDL_ERR_NULL;
+    if (!aligned(a, 16) || !aligned(a_scale, 16) || !aligned(b, 16) || !aligned(b_scale, 16) || !aligned(y, 16)) return CDL_ERR_ALIGN;
+    const int rc = check_ws(ws, ws_bytes, block8_gemm_workspace_bytes(M, N, K));
+    if (rc != CDL_OK) return rc;
+    return launch_block8_gemm(a, a_scale, b, b_scale, M, N, K, a_format, b_format, y, y_type, ws, (hipStream_t)hip_stream);
+}
+
+namespace {
+// 256 rows of an operand (of states, of the vocabulary, or of tokens) within 32-bit offsets; tiles of the logits counted in 32 bits
+bool head_ok(int32_t T, int32_t V, int32_t D) { return D <= 1 << 20 && T <= 1 << 22 && V <= 1 << 30 && (int64_t)T * V <= (int64_t)1 << 44; }
+}
+
+size_t cdl_head_loss_workspace_bytes(int32_t T, int32_t V, int32_t D, int32_t type, int32_t train)
+{
+    if (T < 0 || V < 0 || D < 0 || !head_ok(T, V, D) || !type_ok(type)) return 0;
+    return head_loss_workspace_bytes(T, V, D, type, train != 0);
+}
+
+namespace {
+int check_head(const void *h, const void *w, int32_t type, const int64_t *target, int32_t T, int32_t V, int32_t D)
+{
+    if (T < 0 || V < 0 || D < 0 || !type_ok(type) || (T > 0 && V < 1)) return CDL_ERR_PARAM;
+    if (!head_ok(T, V, D)) return CDL_ERR_RANGE;
+    if (T > 0 && (!target || (D > 0 && (!h || !w)))) return CDL_ERR_NULL;
+    if (!aligned(h, 16) || !aligned(w, 16) || !aligned(target, 8)) return CDL_ERR_ALIGN;
+    return CDL_OK;
+}
+}
+
+int cdl_head_loss_fwd(const void *h, const void *w, int32_t type, const int64_t *target, int32_t T, int32_t V, int32_t D,
+                      float *loss, float *lse, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    int rc = check_head(h, w, type, target, T, V, D);
+    if (rc != CDL_OK) return rc;
+    if (T > 0 && !lse) return CDL_ERR_NULL;
+    if (!aligned(loss, 4) || !aligned(lse, 4)) return CDL_ERR_ALIGN;
+    rc = check_ws(ws, ws_bytes, head_loss_workspace_bytes(T, V, D, type, false));
+    if (rc != CDL_OK) return rc;
+    return launch_head_loss_fwd(h, w, type, target, T, V, D, loss, lse, ws, (hipStream_t)hip_stream);
+}
+
+int cdl_head_loss_bwd(const void *h, const void *w, int32_t type, const int64_t *target, const float *lse,
+                      const float *d_loss, const float *d_lse, int32_t T, int32_t V, int32_t D,
+                      void *d_h, void *d_w, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    int rc = check_head(h, w, type, target, T, V, D);
+    if (rc != CDL_OK) return rc;
+    if ((!d_h && !d_w) || (T > 0 && !lse)) return CDL_ERR_NULL;
+    if (!aligned(lse, 4) || !aligned(d_loss, 4) || !aligned(d_lse, 4) || !aligned(d_h, 16) || !aligned(d_w, 16)) return CDL_ERR_ALIGN;
+    rc = check_ws(ws, ws_bytes, head_loss_workspace_bytes(T, V, D, type, true));
+    if (rc != CDL_OK) return rc;
+    return launch_head_loss_bwd(h, w, type, target, lse, d_loss, d_lse, T, V, D, d_h, d_w, ws, (hipStream_t)hip_stream);
+}
+
+int cdl_dropout(const void *x, const void *add, int32_t type, int64_t n, float p, uint64_t seed, uint64_t counter, void *y, void *hip_stream)
+{
+    if (n < 0 || n > (int64_t)1 << 40 || !type_ok(type) || !(p >= 0.0f && p <= 1.0f)) return CDL_ERR_PARAM;
+    if (n > 0 && (!x || !y)) return CDL_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(add, 16) || !aligned(y, 16)) return CDL_ERR_ALIGN;
+    return launch_dropout(x, add, type, n, p, seed, counter, y, (hipStream_t)hip_stream);
+}
+
 int cdl_probe_mfma_int8(int32_t iters, int32_t random_operands, int32_t blocks, void *sink, double *ops, void *hip_stream)
 {
     if (iters < 1 || blocks < 1 || !sink) return iters < 1 || blocks < 1 ? CDL_ERR_PARAM : CDL_ERR_NULL;

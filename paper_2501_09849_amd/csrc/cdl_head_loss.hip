@@ -1,0 +1,614 @@
+// Softmax cross entropy of a linear last layer over a large vocabulary, its logits never in memory as a whole, and its gradients.
+#include <cmath>
+
+#include "cdl_ring.h"
+
+namespace cdl {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+using Wide = RingForm<2, 2, 4, 4, 4, 1, 8192>;        // 256 x 256
+using Square = RingForm<2, 2, 2, 2, 4, 2, 4096>;      // 128 x 128
+using Thin = RingForm<4, 1, 1, 2, 5, 2, 4096>;        // 128 x 64
+
+// The logit of a token's target, where it lies in the wave's part of a tile (entry `at` of its 32 TP): the one that the sums are made of, so that a sure
+// token's loss and gradient vanish.  Few parts hold any: the search is skipped there.  Every lane stores f(logit), those without a target to `spare`: no
+// branch that lanes take apart, around which the compiler would have to move registers that hold addresses.
+template <class FORM, class F>
+__device__ __forceinline__ void find_target(const v16f (&acc)[FORM::TP][FORM::TQ], int j, int64_t at, int half, float *to, float *spare, const F &f)
+{
+    const bool here = at >= 0 && at < FORM::TP * 32 && ((int)(at >> 2) & 1) == half;
+    if (__builtin_amdgcn_ballot_w64(here) == 0) return;
+    const int own = (int)at - 4 * half;
+    float z = 0.0f;
+#pragma unroll
+    for (int i = 0; i < FORM::TP; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z = i * 32 + 8 * (r >> 2) + (r & 3) == own ? acc[i][j][r] : z;
+    *(here ? to : spare) = f(z);
+}
+
+// ---- the logits of a tile, reduced to the largest and the sum of exponentials of every token --------------------------
+
+template <class FORM>
+struct Reduce {
+    static constexpr int kStores = FORM::TQ / 2;
+    float2 *partial;      // [ceil(V / (32 TP))][T]: the largest logit of a stretch of the vocabulary, and the sum of exp(z - largest)
+    const int64_t *target;
+    float *at_target;     // [T] and one to spare: the logit of the target
+    int V, T;
+    __device__ __forceinline__ void operator()(const v16f (&acc)[FORM::TP][FORM::TQ], int p0, int q0, int, uint8_t *, int lane) const
+    {
+        if (p0 + FORM::TP * 32 <= V) columns<true>(acc, p0, q0, lane);
+        else if (p0 < V) columns<false>(acc, p0, q0, lane);
+        __builtin_amdgcn_s_waitcnt(wait_imm(0));
+    }
+    template <bool FULL>
+    __device__ __forceinline__ void columns(const v16f (&acc)[FORM::TP][FORM::TQ], int p0, int q0, int lane) const
+    {
+        constexpr int TP = FORM::TP, TQ = FORM::TQ;
+        const int row = lane & 31, half = lane >> 5, left = V - p0 - 4 * half;
+        float2 *const out = partial + (int64_t)(p0 / (TP * 32)) * T;
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) {
+            float m = -INFINITY, s = 0.0f;
+            auto value = [&](int i, int r) { return FULL || i * 32 + 8 * (r >> 2) + (r & 3) < left ? acc[i][j][r] : -INFINITY; };
+#pragma unroll
+            for (int i = 0; i < TP; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) m = fmaxf(m, value(i, r));
+            m = fmaxf(m, __shfl_xor(m, 32, 64));
+            const float shift = -m * kLog2e;
+#pragma unroll
+            for (int i = 0; i < TP; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f(__builtin_fmaf(value(i, r), kLog2e, shift));
+            s += __shfl_xor(s, 32, 64);
+            const int t = q0 + j * 32 + row;
+            if (half == 0 && t < T) out[t] = make_float2(m, s);
+            const int64_t to = t < T ? target[t] : -1;
+            find_target<FORM>(acc, j, to < V ? to - p0 : -1, half, at_target + t, at_target + T, [](float z) { return z; });
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
+
+template <class FORM, bool PARTS>
+__global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
+void head_reduce_kernel(RingJob job, Reduce<FORM> reduce)
+{
+    ring<FORM, OpBf16, PARTS>(job, reduce);
+}
+
+// A block: 16 tokens, whose stretches 64 threads each add up.
+constexpr int kFinishTokens = 16, kFinishThreads = 1024;
+__global__ __launch_bounds__(kFinishThreads)
+void head_finish_kernel(const float2 *__restrict__ partial, int stretches, const float *__restrict__ at_target, const int64_t *__restrict__ target, int tokens, int V,
+                        float *__restrict__ loss, float *__restrict__ lse)
+{
+    __shared__ float2 part[64][kFinishTokens];
+    const int tid = threadIdx.x, own = tid & 15, group = tid >> 4, t = blockIdx.x * kFinishTokens + own;
+    float m = -INFINITY, s = 0.0f;
+    if (t < tokens)
+        for (int i = group; i < stretches; i += 64) {
+            const float2 x = partial[(int64_t)i * tokens + t];
+            const float top = fmaxf(m, x.x);
+            // (equal largest ones, also infinite: no difference of infinities)
+            s = s * (m == top ? 1.0f : expf(m - top)) + x.y * (x.x == top ? 1.0f : expf(x.x - top));
+            m = top;
+        }
+    part[group][own] = make_float2(m, s);
+    __syncthreads();
+    if (group != 0 || t >= tokens) return;
+    float top = -INFINITY, sum = 0.0f;
+    for (int g = 0; g < 64; ++g) top = fmaxf(top, part[g][own].x);
+    for (int g = 0; g < 64; ++g) {
+        const float2 x = part[g][own];
+        sum += x.y * (x.x == top ? 1.0f : expf(x.x - top));
+    }
+    const float all = top + logf(sum);
+    lse[t] = all;
+    if (loss) {
+        const int64_t at = target[t];
+        loss[t] = at >= 0 && at < V ? all - at_target[t] : 0.0f;
+    }
+}
+
+// ---- operands -------------------------------------------------------------------------------------------------------
+
+// x[rows, D] as bf16 rows of Dp entries, zeros beyond D; fp32 in three parts [3][rows][Dp] whose sum is x: each the rest rounded to bf16.
+template <class T>
+__global__ __launch_bounds__(256)
+void head_rows_kernel(const T *__restrict__ x, int64_t rows, int D, int Dp, bf16_t *__restrict__ out)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;      // eight entries
+    const int per = Dp / 8;
+    const int64_t r = i / per;
+    if (r >= rows) return;
+    const int d = (int)(i - r * per) * 8;
+    float v[8];
+    const T *const at = x + r * D + d;
+    if (D % 8 == 0 && d < D) {
+        load8(at, v, false);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = d + k < D ? (float)at[k] : 0.0f;
+    }
+    bf16_t *to = out + r * Dp + d;
+    store8(to, v, false);
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int part = 1; part < 3; ++part) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] -= (float)(bf16_t)v[k];
+            to += rows * Dp;
+            store8(to, v, false);
+        }
+    }
+}
+
+// Rows [rows][ld] -> [cols][ld_out], zeros beyond rows; parts `plane` and `plane_out` entries apart, by blockIdx.z.  ld, ld_out multiples of 64.
+__global__ __launch_bounds__(256)
+void head_transpose_kernel(const bf16_t *__restrict__ x, int64_t ld, int64_t plane, int rows, int cols, bf16_t *__restrict__ out, int64_t ld_out, int64_t plane_out)
+{
+    __shared__ uint16_t tile[64][72];
+    x += blockIdx.z * plane;
+    out += blockIdx.z * plane_out;
+    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tid = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = i * 32 + (tid >> 3), c = (tid & 7) * 8;
+        union { u32x4 u; uint16_t h[8]; } v;
+        v.u = (u32x4){0, 0, 0, 0};
+        if (r0 + r < rows) v.u = *reinterpret_cast<const u32x4 *>(x + (int64_t)(r0 + r) * ld + c0 + c);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) tile[c + k][r] = v.h[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = i * 32 + (tid >> 3), r = (tid & 7) * 8;
+        if (c0 + c < cols) *reinterpret_cast<u32x4 *>(out + (int64_t)(c0 + c) * ld_out + r0 + r) = *reinterpret_cast<const u32x4 *>(&tile[c][r]);
+    }
+}
+
+// ---- gradient of the logits ------------------------------------------------------------------------------------------
+
+// Of a token: the factor of its probabilities and of its target, over `unit`, its log-sum, the target.
+struct Token { float factor, lse; int target; float at_target; };
+
+__global__ __launch_bounds__(1024)
+void head_unit_kernel(const int64_t *__restrict__ target, const float *__restrict__ d_loss, const float *__restrict__ d_lse, int T, int V, float *__restrict__ unit)
+{
+    __shared__ float part[16];
+    float m = 0.0f;
+    for (int t = threadIdx.x; t < T; t += 1024) {
+        const int64_t at = target[t];
+        const float a = at >= 0 && at < V ? (d_loss ? fabsf(d_loss[t]) : 1.0f) : 0.0f, b = d_lse ? fabsf(d_lse[t]) : 0.0f;
+        m = fmaxf(m, a + b);
+    }
+#pragma unroll
+    for (int s = 32; s; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i]);
+        *unit = m > 0.0f && m < INFINITY ? m : 1.0f;
+    }
+}
+
+__global__ __launch_bounds__(256)
+void head_tokens_kernel(const int64_t *__restrict__ target, const float *__restrict__ lse, const float *__restrict__ d_loss, const float *__restrict__ d_lse, int tokens,
+                        int padded, int V, const float *__restrict__ unit, Token *__restrict__ out)
+{
+    const int t = blockIdx.x * 256 + threadIdx.x;
+    if (t >= padded) return;
+    Token k{0.0f, INFINITY, -1, 0.0f};      // (beyond the tokens: probabilities exp(-inf))
+    if (t < tokens) {
+        const int64_t at = target[t];
+        const bool in = at >= 0 && at < V;
+        const float by = *unit, dl = in ? (d_loss ? d_loss[t] : 1.0f) : 0.0f;
+        k.lse = lse[t];
+        k.factor = (dl + (d_lse ? d_lse[t] : 0.0f)) / by;
+        k.target = in ? (int)at : -1;
+        k.at_target = dl / by;
+    }
+    out[t] = k;
+}
+
+// g of a piece of the vocabulary, [T][ld], zeros from `cols` up to ld; PARTS: in three parts `plane` entries apart
+template <class FORM, bool PARTS>
+struct Gradient {
+    static constexpr int kStores = row_stores<FORM, bf16_t>();
+    RowTarget<bf16_t> to;
+    const Token *tokens;      // padded to whole tiles
+    float *at_target;         // [T] and one to spare: the probability of the target, where it lies in the piece
+    int T, first, cols;       // first: of the piece, in the vocabulary
+    int64_t plane;
+    __device__ __forceinline__ static float probability(float z, float lse)
+    {
+        if (!PARTS) return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -lse));      // (lse times log2 e)
+        // the rounding of the product with log2 e goes into a second factor
+        const float e = z - lse, hi = e * kLog2e, lo = __builtin_fmaf(e, kLog2e, -hi) + e * 1.925963033500703e-8f, x = __builtin_amdgcn_exp2f(hi);
+        return e > -INFINITY ? __builtin_fmaf(x, lo * 0.69314718055994530942f, x) : 0.0f;
+    }
+    __device__ __forceinline__ void operator()(const v16f (&acc)[FORM::TP][FORM::TQ], int p0, int q0, int, uint8_t *staging, int lane) const
+    {
+        const int half = lane >> 5, left = p0 + FORM::TP * 32 <= cols ? FORM::TP * 32 : cols - p0 - 4 * half;
+        float factor[FORM::TQ], lse[FORM::TQ];
+#pragma unroll
+        for (int j = 0; j < FORM::TQ; ++j) {
+            const int t = q0 + j * 32 + (lane & 31);
+            const Token k = tokens[t];
+            factor[j] = k.factor;
+            lse[j] = PARTS ? k.lse : k.lse * kLog2e;
+            find_target<FORM>(acc, j, k.target < 0 ? -1 : (int64_t)k.target - first - p0, half, at_target + t, at_target + T,
+                              [&](float z) { return probability(z, lse[j]); });
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        auto g = [&](float z, int p, int j) {
+            const float x = probability(z, lse[j]) * factor[j];
+            return p < left ? x : 0.0f;
+        };
+        store_rows<FORM, bf16_t, false>(acc, to, p0, q0, staging, lane, g);
+        if (PARTS) {
+            RowTarget<bf16_t> at = to;
+            at.out += plane;
+            store_rows<FORM, bf16_t, false>(acc, at, p0, q0, staging, lane, [&](float z, int p, int j) { const float x = g(z, p, j); return x - (float)(bf16_t)x; });
+            at.out += plane;
+            store_rows<FORM, bf16_t, false>(acc, at, p0, q0, staging, lane, [&](float z, int p, int j) {
+                const float x = g(z, p, j), y = x - (float)(bf16_t)x;
+                return y - (float)(bf16_t)y;
+            });
+        }
+    }
+};
+
+template <class FORM, bool PARTS>
+__global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
+void head_gradient_kernel(RingJob job, Gradient<FORM, PARTS> gradient)
+{
+    ring<FORM, OpBf16, PARTS>(job, gradient);
+}
+
+// the targets: what is left out above
+__global__ __launch_bounds__(256)
+void head_target_kernel(const Token *__restrict__ tokens, const float *__restrict__ at_target, int T, int v0, int cols, bf16_t *__restrict__ g, int64_t ld, int64_t plane, int parts)
+{
+    const int t = blockIdx.x * 256 + threadIdx.x;
+    if (t >= T) return;
+    const Token k = tokens[t];
+    const int v = k.target - v0;
+    if (k.target < 0 || v < 0 || v >= cols) return;
+    float x = k.factor * at_target[t] - k.at_target;
+    for (int i = 0; i < parts; ++i) {
+        const bf16_t part = (bf16_t)x;
+        g[i * plane + (int64_t)t * ld + v] = part;
+        x -= (float)part;
+    }
+}
+
+// ---- products with it -------------------------------------------------------------------------------------------------
+
+// by: results times *by; ADD: onto what is there; parts of a split contraction `part` entries apart
+template <class FORM, class T, bool ADD>
+struct Store {
+    static constexpr int kStores = row_stores<FORM, T>();
+    RowTarget<T> to;
+    int64_t part;
+    const float *by;
+    __device__ __forceinline__ void operator()(const v16f (&acc)[FORM::TP][FORM::TQ], int p0, int q0, int split, uint8_t *staging, int lane) const
+    {
+        RowTarget<T> at = to;
+        at.out += split * part;
+        const float scale = by ? *by : 1.0f;
+        store_rows<FORM, T, ADD>(acc, at, p0, q0, staging, lane, [&](float v, int, int) { return v * scale; });
+    }
+};
+
+template <class FORM, bool PARTS, class T, bool ADD>
+__global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
+void head_product_kernel(RingJob job, Store<FORM, T, ADD> store)
+{
+    ring<FORM, OpBf16, PARTS>(job, store);
+}
+
+template <class T>
+__global__ __launch_bounds__(256)
+void head_sum_kernel(const float *__restrict__ parts, int splits, int64_t n, const float *__restrict__ by, T *__restrict__ y)
+{
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= n) return;
+    float sum = 0.0f;
+    for (int s = 0; s < splits; ++s) sum += parts[s * n + e];
+    y[e] = (T)(sum * *by);
+}
+
+template <class T>
+__global__ __launch_bounds__(256)
+void head_zero_kernel(T *y, int64_t n)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) y[i] = (T)0.0f;
+}
+
+// ---- layouts ----------------------------------------------------------------------------------------------------------
+
+enum Form { kWide, kSquare, kThin };
+constexpr int form_p(Form f) { return f == kWide ? 256 : 128; }
+constexpr int form_q(Form f) { return f == kWide ? 256 : f == kSquare ? 128 : 64; }
+constexpr int form_per_cu(Form f) { return f == kWide ? 1 : 2; }
+constexpr int form_stretch(Form f) { return f == kWide ? 128 : f == kSquare ? 64 : 32; }      // entries of P of a wave
+
+Form choose_form(int64_t rows_p, int64_t rows_q)
+{
+    if (rows_q <= 64) return kThin;
+    return ((rows_p + 255) / 256) * ((rows_q + 255) / 256) >= 128 ? kWide : kSquare;
+}
+
+int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by * by; }
+
+struct Split { int splits, k_per; };
+Split choose_splits(int64_t tiles, int per_cu, int nk)
+{
+    const int pairs = nk / 2;
+    int64_t s = 256 * per_cu / tiles;
+    s = s < pairs / 4 ? s : pairs / 4;
+    if (s < 1) s = 1;
+    const int per = (int)((pairs + s - 1) / s);
+    return {(pairs + per - 1) / per, 2 * per};
+}
+
+// Entries of g that are in memory at a time: 256 MB of bf16, which the memory-side cache holds.
+constexpr int64_t kPieceEntries = 1 << 27;
+
+struct Plan {
+    int parts;
+    int64_t Dp, Tp;                   // up to multiples of 64
+    bool copy;                        // the operands as rows of Dp entries in the workspace
+    Form reduce;
+    int64_t stretches;
+    // training
+    int64_t piece, piece_p;           // entries of the vocabulary at a time, up to a multiple of 64
+    Form gradient, form_h, form_w;
+    Split split_h;
+    int64_t tokens;                   // of the table, whole tiles
+    // offsets in the workspace
+    size_t rows_h, rows_w, at_target, partial, unit, table, ht, wt, g, gt, sums, bytes;
+};
+
+Plan make_plan(int64_t T, int64_t V, int64_t D, int32_t type, bool train)
+{
+    Plan p{};
+    p.parts = type == CDL_F32 ? 3 : 1;
+    p.Dp = D == 0 ? 64 : up(D, 64);
+    p.Tp = up(T, 64);
+    p.copy = type == CDL_F32 || p.Dp != D;
+    p.reduce = choose_form(V, T);
+    p.stretches = (V + form_stretch(p.reduce) - 1) / form_stretch(p.reduce);
+    size_t at = 0;
+    auto take = [&](int64_t bytes) { const size_t here = at; at += align_up((size_t)bytes, 256); return here; };
+    if (p.copy) {
+        p.rows_h = take(p.parts * T * p.Dp * 2);
+        p.rows_w = take(p.parts * V * p.Dp * 2);
+    }
+    p.at_target = take((T + 1) * 4);
+    const size_t kept = at;
+    p.partial = take(p.stretches * T * 8);
+    if (train) {
+        const size_t forward = at;
+        at = kept;      // the sums of the forward call are not needed any more
+        p.unit = take(256);
+        p.tokens = up(T, 256);
+        p.table = take(p.tokens * (int64_t)sizeof(Token));
+        int64_t most = up(kPieceEntries / (T < 1 ? 1 : T) / p.parts, 2048);
+        most = most < 2048 ? 2048 : most > 1 << 22 ? 1 << 22 : most;      // (256 rows of g transposed within 32-bit offsets)
+        const int64_t pieces = (V + most - 1) / most;
+        p.piece = pieces == 1 ? V : up((V + pieces - 1) / pieces, 256);
+        p.piece_p = up(p.piece, 64);
+        p.gradient = choose_form(p.piece, T);
+        p.form_h = choose_form(D, T);
+        p.form_w = choose_form(D, p.piece);
+        const int64_t tiles = ((D + form_p(p.form_h) - 1) / form_p(p.form_h)) * ((T + form_q(p.form_h) - 1) / form_q(p.form_h));
+        p.split_h = choose_splits(tiles < 1 ? 1 : tiles, form_per_cu(p.form_h), (int)(p.piece_p / 32 * (p.parts == 3 ? 6 : 1)));
+        p.ht = take(p.parts * up(D, 64) * p.Tp * 2);
+        p.wt = take(p.parts * up(D, 64) * p.piece_p * 2);
+        p.g = take(p.parts * T * p.piece_p * 2);
+        p.gt = take(p.parts * p.piece_p * p.Tp * 2);
+        p.sums = take((int64_t)p.split_h.splits * T * D * 4);
+        if (at < forward) at = forward;
+    }
+    p.bytes = at;
+    return p;
+}
+
+unsigned blocks_of(int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); }
+
+template <class KERNEL, class EPILOGUE>
+int launch_ring(const char *name, KERNEL kernel, int lds, int threads, int per_cu, const RingJob &job, const EPILOGUE &e, hipStream_t stream)
+{
+    const hipError_t err = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (err != hipSuccess) return hip_failed(err);
+    const int64_t grid = ring_blocks((int64_t)job.tiles_p * job.tiles_q * job.splits, per_cu);
+    CDL_LAUNCH(name, stream, kernel, dim3((unsigned)grid), dim3((unsigned)threads), lds, job, e);
+    return check_launch();
+}
+#define CDL_RING(NAME, FORM, KERNEL, JOB, E, STREAM) launch_ring(NAME, KERNEL, FORM::kLds, FORM::kThreads, FORM::PER_CU, JOB, E, STREAM)
+
+RingJob ring_job(Form form, const void *P, int64_t ldp, int64_t rows_p, const void *Q, int64_t ldq, int64_t rows_q, int64_t entries, int parts, int64_t plane_p, int64_t plane_q)
+{
+    RingJob job{};
+    job.P = (const uint8_t *)P;
+    job.Q = (const uint8_t *)Q;
+    job.ldp = ldp * 2;
+    job.ldq = ldq * 2;
+    job.rowsP = (int)rows_p;
+    job.rowsQ = (int)rows_q;
+    job.plane_nk = (int)(entries / 32);
+    job.nk = job.plane_nk * (parts == 3 ? 6 : 1);
+    job.plane_p = plane_p * 2;
+    job.plane_q = plane_q * 2;
+    job.tiles_p = (int)((rows_p + form_p(form) - 1) / form_p(form));
+    job.tiles_q = (int)((rows_q + form_q(form) - 1) / form_q(form));
+    job.splits = 1;
+    job.k_per = job.nk;
+    return job;
+}
+
+template <bool PARTS>
+int run_reduce(const Plan &p, const RingJob &job, float2 *partial, const int64_t *target, float *at_target, int V, int T, hipStream_t stream)
+{
+    switch (p.reduce) {
+        case kWide: return CDL_RING("head_reduce_kernel", Wide, (head_reduce_kernel<Wide, PARTS>), job, (Reduce<Wide>{partial, target, at_target, V, T}), stream);
+        case kSquare: return CDL_RING("head_reduce_kernel", Square, (head_reduce_kernel<Square, PARTS>), job, (Reduce<Square>{partial, target, at_target, V, T}), stream);
+        default: return CDL_RING("head_reduce_kernel", Thin, (head_reduce_kernel<Thin, PARTS>), job, (Reduce<Thin>{partial, target, at_target, V, T}), stream);
+    }
+}
+
+template <bool PARTS>
+int run_gradient(const Plan &p, const RingJob &job, const RowTarget<bf16_t> &to, const Token *tokens, float *at_target, int T, int first, int cols, int64_t plane, hipStream_t stream)
+{
+    switch (p.gradient) {
+        case kWide: return CDL_RING("head_gradient_kernel", Wide, (head_gradient_kernel<Wide, PARTS>), job, (Gradient<Wide, PARTS>{to, tokens, at_target, T, first, cols, plane}), stream);
+        case kSquare: return CDL_RING("head_gradient_kernel", Square, (head_gradient_kernel<Square, PARTS>), job, (Gradient<Square, PARTS>{to, tokens, at_target, T, first, cols, plane}), stream);
+        default: return CDL_RING("head_gradient_kernel", Thin, (head_gradient_kernel<Thin, PARTS>), job, (Gradient<Thin, PARTS>{to, tokens, at_target, T, first, cols, plane}), stream);
+    }
+}
+
+template <bool PARTS, class T, bool ADD>
+int run_product(Form form, const RingJob &job, const RowTarget<T> &to, int64_t part, const float *by, hipStream_t stream)
+{
+    switch (form) {
+        case kWide: return CDL_RING("head_product_kernel", Wide, (head_product_kernel<Wide, PARTS, T, ADD>), job, (Store<Wide, T, ADD>{to, part, by}), stream);
+        case kSquare: return CDL_RING("head_product_kernel", Square, (head_product_kernel<Square, PARTS, T, ADD>), job, (Store<Square, T, ADD>{to, part, by}), stream);
+        default: return CDL_RING("head_product_kernel", Thin, (head_product_kernel<Thin, PARTS, T, ADD>), job, (Store<Thin, T, ADD>{to, part, by}), stream);
+    }
+}
+
+#define CDL_TRY(X) do { const int cdl_rc_ = (X); if (cdl_rc_ != CDL_OK) return cdl_rc_; } while (0)
+
+template <class T>
+int to_rows(const T *x, int64_t rows, int64_t D, int64_t Dp, bf16_t *out, hipStream_t stream)
+{
+    CDL_LAUNCH("head_rows_kernel", stream, head_rows_kernel<T>, dim3(blocks_of(rows * (Dp / 8), 256)), dim3(256), 0, x, rows, (int)D, (int)Dp, out);
+    return check_launch();
+}
+
+int transpose(const bf16_t *x, int64_t ld, int64_t plane, int64_t rows, int64_t cols, bf16_t *out, int64_t ld_out, int64_t plane_out, int parts, hipStream_t stream)
+{
+    CDL_LAUNCH("head_transpose_kernel", stream, head_transpose_kernel, dim3(blocks_of(cols, 64), blocks_of(rows, 64), (unsigned)parts), dim3(256), 0, x, ld, plane, (int)rows,
+               (int)cols, out, ld_out, plane_out);
+    return check_launch();
+}
+
+template <class T>
+int forward(const T *h, const T *w, int32_t type, const int64_t *target, int32_t tokens, int32_t V, int32_t D, float *loss, float *lse, char *ws, hipStream_t stream)
+{
+    const Plan p = make_plan(tokens, V, D, type, false);
+    const bf16_t *ph = (const bf16_t *)h, *pw = (const bf16_t *)w;
+    if (p.copy) {
+        CDL_TRY(to_rows(h, tokens, D, p.Dp, (bf16_t *)(ws + p.rows_h), stream));
+        CDL_TRY(to_rows(w, V, D, p.Dp, (bf16_t *)(ws + p.rows_w), stream));
+        ph = (const bf16_t *)(ws + p.rows_h);
+        pw = (const bf16_t *)(ws + p.rows_w);
+    }
+    float2 *const partial = (float2 *)(ws + p.partial);
+    const RingJob job = ring_job(p.reduce, pw, p.Dp, V, ph, p.Dp, tokens, p.Dp, p.parts, V * p.Dp, tokens * p.Dp);
+    float *const at_target = (float *)(ws + p.at_target);
+    CDL_TRY(run_reduce<sizeof(T) == 4>(p, job, partial, target, at_target, V, tokens, stream));
+    CDL_LAUNCH("head_finish_kernel", stream, head_finish_kernel, dim3(blocks_of(tokens, kFinishTokens)), dim3(kFinishThreads), 0, (const float2 *)partial,
+               (int)p.stretches, (const float *)at_target, target, tokens, V, loss, lse);
+    return check_launch();
+}
+
+template <class T>
+int backward(const T *h, const T *w, int32_t type, const int64_t *target, const float *lse, const float *d_loss, const float *d_lse, int32_t tokens, int32_t V,
+             int32_t D, T *d_h, T *d_w, char *ws, hipStream_t stream)
+{
+    constexpr bool PARTS = sizeof(T) == 4;
+    const Plan p = make_plan(tokens, V, D, type, true);
+    const bf16_t *ph = (const bf16_t *)h, *pw = (const bf16_t *)w;
+    if (p.copy) {
+        CDL_TRY(to_rows(h, tokens, D, p.Dp, (bf16_t *)(ws + p.rows_h), stream));
+        CDL_TRY(to_rows(w, V, D, p.Dp, (bf16_t *)(ws + p.rows_w), stream));
+        ph = (const bf16_t *)(ws + p.rows_h);
+        pw = (const bf16_t *)(ws + p.rows_w);
+    }
+    float *const unit = (float *)(ws + p.unit), *const at_target = (float *)(ws + p.at_target), *const sums = (float *)(ws + p.sums);
+    Token *const table = (Token *)(ws + p.table);
+    CDL_LAUNCH("head_unit_kernel", stream, head_unit_kernel, dim3(1), dim3(1024), 0, target, d_loss, d_lse, tokens, V, unit);
+    CDL_LAUNCH("head_tokens_kernel", stream, head_tokens_kernel, dim3(blocks_of(p.tokens, 256)), dim3(256), 0, target, lse, d_loss, d_lse, tokens, (int)p.tokens, V,
+               (const float *)unit, table);
+    CDL_TRY(check_launch());
+    bf16_t *const ht = (bf16_t *)(ws + p.ht), *const wt = (bf16_t *)(ws + p.wt), *const g = (bf16_t *)(ws + p.g), *const gt = (bf16_t *)(ws + p.gt);
+    if (d_w) CDL_TRY(transpose(ph, p.Dp, tokens * p.Dp, tokens, D, ht, p.Tp, up(D, 64) * p.Tp, p.parts, stream));
+    const int64_t plane_g = tokens * p.piece_p;
+    for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
+        const int64_t cols = v0 + p.piece <= V ? p.piece : V - v0, padded = up(cols, 64);
+        const bf16_t *const piece = pw + v0 * p.Dp;
+        {
+            const RingJob job = ring_job(p.gradient, piece, p.Dp, cols, ph, p.Dp, tokens, p.Dp, p.parts, V * p.Dp, tokens * p.Dp);
+            CDL_TRY(run_gradient<PARTS>(p, job, RowTarget<bf16_t>{g, p.piece_p, (int)padded, tokens, 16}, table, at_target, tokens, (int)v0, (int)cols, plane_g, stream));
+            CDL_LAUNCH("head_target_kernel", stream, head_target_kernel, dim3(blocks_of(tokens, 256)), dim3(256), 0, (const Token *)table, (const float *)at_target, tokens, (int)v0, (int)cols, g, p.piece_p,
+                       plane_g, p.parts);
+            CDL_TRY(check_launch());
+        }
+        if (d_h) {
+            CDL_TRY(transpose(piece, p.Dp, V * p.Dp, cols, D, wt, p.piece_p, up(D, 64) * p.piece_p, p.parts, stream));
+            RingJob job = ring_job(p.form_h, wt, p.piece_p, D, g, p.piece_p, tokens, padded, p.parts, up(D, 64) * p.piece_p, plane_g);
+            const int pairs = job.nk / 2, k_per = p.split_h.k_per;
+            job.k_per = k_per;
+            job.splits = (2 * pairs + k_per - 1) / k_per;      // (a last, shorter piece: fewer parts)
+            const RowTarget<float> to{sums, D, D, tokens, row_width(sums, (int64_t)D * 4)};
+            const int64_t part = (int64_t)tokens * D;
+            CDL_TRY(v0 == 0 ? (run_product<PARTS, float, false>(p.form_h, job, to, part, nullptr, stream)) : (run_product<PARTS, float, true>(p.form_h, job, to, part, nullptr, stream)));
+        }
+        if (d_w) {
+            CDL_TRY(transpose(g, p.piece_p, plane_g, tokens, cols, gt, p.Tp, p.piece_p * p.Tp, p.parts, stream));
+            const RingJob job = ring_job(p.form_w, ht, p.Tp, D, gt, p.Tp, cols, p.Tp, p.parts, up(D, 64) * p.Tp, p.piece_p * p.Tp);
+            T *const out = d_w + v0 * D;
+            CDL_TRY((run_product<PARTS, T, false>(p.form_w, job, RowTarget<T>{out, D, D, (int)cols, row_width(out, (int64_t)D * (int64_t)sizeof(T))}, 0, unit, stream)));
+        }
+    }
+    if (d_h) {
+        const int64_t n = (int64_t)tokens * D;
+        CDL_LAUNCH("head_sum_kernel", stream, head_sum_kernel<T>, dim3(blocks_of(n, 256)), dim3(256), 0, (const float *)sums, p.split_h.splits, n, (const float *)unit, d_h);
+    }
+    return check_launch();
+}
+
+template <class T>
+int zero(T *y, int64_t n, hipStream_t stream)
+{
+    if (!y || n == 0) return CDL_OK;
+    CDL_LAUNCH("head_zero_kernel", stream, head_zero_kernel<T>, dim3(blocks_of(n, 256)), dim3(256), 0, y, n);
+    return check_launch();
+}
+
+}  // namespace
+
+size_t head_loss_workspace_bytes(int32_t T, int32_t V, int32_t D, int32_t type, bool train)
+{
+    return T == 0 || V == 0 ? 0 : make_plan(T, V, D, type, train).bytes;
+}
+
+int launch_head_loss_fwd(const void *h, const void *w, int32_t type, const int64_t *target, int32_t T, int32_t V, int32_t D, float *loss, float *lse, void *ws,
+                         hipStream_t stream)
+{
+    if (T == 0) return CDL_OK;
+    return type == CDL_BF16 ? forward((const bf16_t *)h, (const bf16_t *)w, type, target, T, V, D, loss, lse, (char *)ws, stream)
+                            : forward((const float *)h, (const float *)w, type, target, T, V, D, loss, lse, (char *)ws, stream);
+}
+
+int launch_head_loss_bwd(const void *h, const void *w, int32_t type, const int64_t *target, const float *lse, const float *d_loss, const float *d_lse,
+                         int32_t T, int32_t V, int32_t D, void *d_h, void *d_w, void *ws, hipStream_t stream)
+{
+    const int64_t n_w = (int64_t)V * D;
+    if (D == 0) return CDL_OK;
+    if (T == 0) return type == CDL_BF16 ? zero((bf16_t *)d_w, n_w, stream) : zero((float *)d_w, n_w, stream);
+    return type == CDL_BF16 ? backward((const bf16_t *)h, (const bf16_t *)w, type, target, lse, d_loss, d_lse, T, V, D, (bf16_t *)d_h, (bf16_t *)d_w, (char *)ws, stream)
+                            : backward((const float *)h, (const float *)w, type, target, lse, d_loss, d_lse, T, V, D, (float *)d_h, (float *)d_w, (char *)ws, stream);
+}
+
+}  // namespace cdl

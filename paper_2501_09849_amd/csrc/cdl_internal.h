@@ -224,6 +224,20 @@ size_t huffman_workspace_bytes(int64_t n);
 int launch_huffman_bits(const int8_t *idx, int64_t n, int lo, int n_levels, unsigned long long *counts,
                         unsigned long long *total_bits, float *bits_per_entry, void *ws, hipStream_t stream);
 
+// ---- layers in 8-bit floating point, the loss, dropout -------------------------------------
+int64_t block8_pitch(int32_t n);
+int launch_block8_quantize(const void *x, int32_t type, int32_t rows, int32_t cols, int32_t tiles, int32_t format, uint8_t *q, uint8_t *scale, uint8_t *q_t,
+                           uint8_t *scale_t, hipStream_t stream);      // (cdl_block8.hip)
+size_t block8_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K);
+int launch_block8_gemm(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale, int32_t M, int32_t N, int32_t K, int32_t a_format,
+                       int32_t b_format, void *y, int32_t y_type, void *ws, hipStream_t stream);      // (cdl_block8_gemm.hip)
+size_t head_loss_workspace_bytes(int32_t T, int32_t V, int32_t D, int32_t type, bool train);
+int launch_head_loss_fwd(const void *h, const void *w, int32_t type, const int64_t *target, int32_t T, int32_t V, int32_t D, float *loss, float *lse, void *ws,
+                         hipStream_t stream);      // (cdl_head_loss.hip)
+int launch_head_loss_bwd(const void *h, const void *w, int32_t type, const int64_t *target, const float *lse, const float *d_loss, const float *d_lse,
+                         int32_t T, int32_t V, int32_t D, void *d_h, void *d_w, void *ws, hipStream_t stream);
+int launch_dropout(const void *x, const void *add, int32_t type, int64_t n, float p, uint64_t seed, uint64_t counter, void *y, hipStream_t stream);      // (cdl_dropout.hip)
+
 int launch_mfma_probe(int iters, int random_operands, int blocks, int *sink, hipStream_t stream);
 
 }  // namespace cdl

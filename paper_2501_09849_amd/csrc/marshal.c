@@ -100,11 +100,12 @@ static int get_real(PyObject *o, float *v)
 /*
  * One call's arguments by the letters of a format: p pointer, n 64-bit size, i 32-bit size, o offset (among the 32-bit
  * integers), f float, r real number by float() (among the floats), q quantizer (lo, n_levels, delta, alpha, top_k: five
- * arguments), w workspace (pointer and size), s stream.  They are filled in order into the arrays of their kind.
+ * arguments), u unsigned 64-bit number, w workspace (pointer and size), s stream.  They are filled in order into the arrays of their kind.
  */
 struct args {
     void *p[12];
     int64_t n;
+    uint64_t u[2];
     int32_t i[12];
     float f[2];
     cdl_qparams q[2];
@@ -115,7 +116,7 @@ struct args {
 
 static int parse(const char *name, const char *format, PyObject *const *o, Py_ssize_t count, struct args *a)
 {
-    int np = 0, ni = 0, nf = 0, nq = 0;
+    int np = 0, ni = 0, nf = 0, nq = 0, nu = 0;
     Py_ssize_t at = 0;
     int64_t v;
     for (const char *c = format; *c; ++c) {
@@ -123,6 +124,10 @@ static int parse(const char *name, const char *format, PyObject *const *o, Py_ss
         switch (*c) {
             case 'p': if (get_ptr(o[at++], &a->p[np++])) return -1; break;
             case 'n': if (get_index(o[at++], &a->n)) return -1; break;
+            case 'u':
+                a->u[nu++] = PyLong_AsUnsignedLongLong(o[at++]);      /* (an integer in [0, 2^64), else an error) */
+                if (PyErr_Occurred()) return -1;
+                break;
             case 'i': if (get_index(o[at++], &v)) return -1; a->i[ni++] = (int32_t)v; break;
             case 'o': if (get_int(o[at++], &v)) return -1; a->i[ni++] = (int32_t)v; break;
             case 'r': if (get_real(o[at++], &a->f[nf++])) return -1; break;
@@ -170,6 +175,15 @@ wrong:
     X(cdl_qconv_bwd_activations, "ppiiiiiiiiifpws",                                                                                     \
       (a.p[0], a.p[1], a.i[0], a.i[1], a.i[2], a.i[3], a.i[4], a.i[5], a.i[6], a.i[7], a.i[8], a.f[0], a.p[2], a.ws, a.ws_bytes,        \
        a.stream))                                                                                                                       \
+    X(cdl_block8_quantize, "piiiiipppps",                                                                                               \
+      (a.p[0], a.i[0], a.i[1], a.i[2], a.i[3], a.i[4], a.p[1], a.p[2], a.p[3], a.p[4], a.stream))                                       \
+    X(cdl_block8_gemm, "ppppiiiiipiws",                                                                                                 \
+      (a.p[0], a.p[1], a.p[2], a.p[3], a.i[0], a.i[1], a.i[2], a.i[3], a.i[4], a.p[4], a.i[5], a.ws, a.ws_bytes, a.stream))             \
+    X(cdl_head_loss_fwd, "ppipiiippws",                                                                                                 \
+      (a.p[0], a.p[1], a.i[0], a.p[2], a.i[1], a.i[2], a.i[3], a.p[3], a.p[4], a.ws, a.ws_bytes, a.stream))                             \
+    X(cdl_head_loss_bwd, "ppippppiiippws",                                                                                              \
+      (a.p[0], a.p[1], a.i[0], a.p[2], a.p[3], a.p[4], a.p[5], a.i[1], a.i[2], a.i[3], a.p[6], a.p[7], a.ws, a.ws_bytes, a.stream))     \
+    X(cdl_dropout, "ppinruups", (a.p[0], a.p[1], a.i[0], a.n, a.f[0], a.u[0], a.u[1], a.p[2], a.stream))                                \
     /* the last integer: whether the weight quantizer is given */                                                                       \
     X(cdl_qgemm_bwd_quantize_bwd, "pppiiipqfopppppiqpppws",                                                                             \
       (a.p[0], a.p[1], a.p[2], a.i[0], a.i[1], a.i[2], a.p[3], &a.q[0], a.f[0], a.i[3], a.p[4], a.p[5], a.p[6], a.p[7], a.p[8],         \

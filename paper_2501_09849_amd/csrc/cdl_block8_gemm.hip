@@ -4,9 +4,9 @@
 namespace cdl {
 namespace {
 
-using Wide = RingForm<2, 2, 4, 4, 4, 1, 4096, true>;        // 256 x 256
-using Square = RingForm<2, 2, 2, 2, 6, 1, 4096, true>;      // 128 x 128
-using Thin = RingForm<4, 1, 1, 2, 5, 2, 4096, true>;        // 128 of b, 64 of a
+using Wide = RingForm<2, 2, 4, 4, 2, 2, 1, 4096, true>;        // 256 x 256
+using Square = RingForm<2, 2, 2, 2, 4, 4, 1, 4096, true>;      // 128 x 128
+using Thin = RingForm<4, 1, 1, 2, 3, 3, 2, 0, true>;           // 128 of b, 64 of a
 
 template <class FORM, class T>
 struct Store {
@@ -67,20 +67,20 @@ struct Layout {
 
 Layout layout(int32_t M, int32_t N, int32_t K)
 {
-    const int pairs = (int)(block8_pitch(K) / 128);      // two K-tiles
+    const int nk = (int)(block8_pitch(K) / kRingRow);
     Layout l;
     const int64_t wide = (int64_t)((M + 255) / 256) * ((N + 255) / 256);
-    l.form = M <= 64 ? kThin : wide * pairs >= 24 * 128 ? kWide : kSquare;
+    l.form = M <= 64 ? kThin : wide * nk >= 24 * 128 ? kWide : kSquare;
     const int p = l.form == kWide ? 256 : 128, q = l.form == kWide ? 256 : l.form == kSquare ? 128 : 64, per_cu = l.form == kThin ? 2 : 1;
     l.tiles_p = (N + p - 1) / p;
     l.tiles_q = (M + q - 1) / q;
     const int64_t tiles = (int64_t)l.tiles_p * l.tiles_q, places = 256 * per_cu;
     int64_t splits = tiles >= places ? 1 : places / tiles;
-    splits = splits < pairs / 4 ? splits : pairs / 4;
+    splits = splits < nk / 4 ? splits : nk / 4;
     if (splits < 1) splits = 1;
-    const int per = (int)((pairs + splits - 1) / splits);
-    l.splits = (pairs + per - 1) / per;
-    l.k_per = 2 * per;
+    const int per = (int)((nk + splits - 1) / splits);
+    l.splits = (nk + per - 1) / per;
+    l.k_per = per;
     return l;
 }
 

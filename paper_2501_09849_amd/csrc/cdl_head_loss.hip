@@ -8,9 +8,9 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
-using Wide = RingForm<2, 2, 4, 4, 4, 1, 8192>;        // 256 x 256
-using Square = RingForm<2, 2, 2, 2, 4, 2, 4096>;      // 128 x 128
-using Thin = RingForm<4, 1, 1, 2, 5, 2, 4096>;        // 128 x 64
+using Wide = RingForm<2, 2, 4, 4, 3, 2, 1>;        // 256 x 256
+using Square = RingForm<2, 2, 2, 2, 3, 2, 2>;      // 128 x 128
+using Thin = RingForm<4, 1, 1, 2, 3, 3, 2>;        // 128 x 64
 
 // The logit of a token's target, where it lies in the wave's part of a tile (entry `at` of its 32 TP): the one that the sums are made of, so that a sure
 // token's loss and gradient vanish.  Few parts hold any: the search is skipped there.  Every lane stores f(logit), those without a target to `spare`: no
@@ -33,7 +33,7 @@ __device__ __forceinline__ void find_target(const v16f (&acc)[FORM::TP][FORM::TQ
 
 template <class FORM>
 struct Reduce {
-    static constexpr int kStores = FORM::TQ / 2;
+    static constexpr int kStores = 0;
     float2 *partial;      // [ceil(V / (32 TP))][T]: the largest logit of a stretch of the vocabulary, and the sum of exp(z - largest)
     const int64_t *target;
     float *at_target;     // [T] and one to spare: the logit of the target
@@ -42,7 +42,6 @@ struct Reduce {
     {
         if (p0 + FORM::TP * 32 <= V) columns<true>(acc, p0, q0, lane);
         else if (p0 < V) columns<false>(acc, p0, q0, lane);
-        __builtin_amdgcn_s_waitcnt(wait_imm(0));
     }
     template <bool FULL>
     __device__ __forceinline__ void columns(const v16f (&acc)[FORM::TP][FORM::TQ], int p0, int q0, int lane) const
@@ -352,12 +351,11 @@ int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by * by; }
 struct Split { int splits, k_per; };
 Split choose_splits(int64_t tiles, int per_cu, int nk)
 {
-    const int pairs = nk / 2;
     int64_t s = 256 * per_cu / tiles;
-    s = s < pairs / 4 ? s : pairs / 4;
+    s = s < nk / 4 ? s : nk / 4;
     if (s < 1) s = 1;
-    const int per = (int)((pairs + s - 1) / s);
-    return {(pairs + per - 1) / per, 2 * per};
+    const int per = (int)((nk + s - 1) / s);
+    return {(nk + per - 1) / per, per};
 }
 
 // Entries of g that are in memory at a time: 256 MB of bf16, which the memory-side cache holds.
@@ -411,7 +409,7 @@ Plan make_plan(int64_t T, int64_t V, int64_t D, int32_t type, bool train)
         p.form_h = choose_form(D, T);
         p.form_w = choose_form(D, p.piece);
         const int64_t tiles = ((D + form_p(p.form_h) - 1) / form_p(p.form_h)) * ((T + form_q(p.form_h) - 1) / form_q(p.form_h));
-        p.split_h = choose_splits(tiles < 1 ? 1 : tiles, form_per_cu(p.form_h), (int)(p.piece_p / 32 * (p.parts == 3 ? 6 : 1)));
+        p.split_h = choose_splits(tiles < 1 ? 1 : tiles, form_per_cu(p.form_h), (int)(p.piece_p / 64 * (p.parts == 3 ? 6 : 1)));
         p.ht = take(p.parts * up(D, 64) * p.Tp * 2);
         p.wt = take(p.parts * up(D, 64) * p.piece_p * 2);
         p.g = take(p.parts * T * p.piece_p * 2);
@@ -445,7 +443,7 @@ RingJob ring_job(Form form, const void *P, int64_t ldp, int64_t rows_p, const vo
     job.ldq = ldq * 2;
     job.rowsP = (int)rows_p;
     job.rowsQ = (int)rows_q;
-    job.plane_nk = (int)(entries / 32);
+    job.plane_nk = (int)(entries / 64);
     job.nk = job.plane_nk * (parts == 3 ? 6 : 1);
     job.plane_p = plane_p * 2;
     job.plane_q = plane_q * 2;
@@ -557,9 +555,8 @@ int backward(const T *h, const T *w, int32_t type, const int64_t *target, const 
         if (d_h) {
             CDL_TRY(transpose(piece, p.Dp, V * p.Dp, cols, D, wt, p.piece_p, up(D, 64) * p.piece_p, p.parts, stream));
             RingJob job = ring_job(p.form_h, wt, p.piece_p, D, g, p.piece_p, tokens, padded, p.parts, up(D, 64) * p.piece_p, plane_g);
-            const int pairs = job.nk / 2, k_per = p.split_h.k_per;
-            job.k_per = k_per;
-            job.splits = (2 * pairs + k_per - 1) / k_per;      // (a last, shorter piece: fewer parts)
+            job.k_per = p.split_h.k_per;
+            job.splits = (job.nk + job.k_per - 1) / job.k_per;      // (a last, shorter piece: fewer parts)
             const RowTarget<float> to{sums, D, D, tokens, row_width(sums, (int64_t)D * 4)};
             const int64_t part = (int64_t)tokens * D;
             CDL_TRY(v0 == 0 ? (run_product<PARTS, float, false>(p.form_h, job, to, part, nullptr, stream)) : (run_product<PARTS, float, true>(p.form_h, job, to, part, nullptr, stream)));

@@ -3,12 +3,14 @@
 //
 //   D[p,q] = sum_k P[p,k] * Q[q,k]
 //
-// A block of threads owns kP x kQ entries of D, its waves TP x TQ accumulators of 32 x 32 each.  K-tiles are 64 bytes of every row of both
-// operands.  They come by direct global->LDS loads through a ring of RING stages, RING - 1 of them under way, across the ends of tiles: a block
-// takes tile after tile as one sequence of K-tiles.  What bounds it is the LDS and the loads, not the matrix cores, wherever a wave's
-// tile is small: a wave reads (32 TP + 32 TQ) * 64 bytes for TP * TQ * 64 cycles of its matrix core, so the widest form has four
-// waves of 128 x 128, whose 256 accumulators leave one wave to a SIMD.  The fragments of a step are therefore read behind
-// the products of the step before, and the products of one step cover the loads of the next.
+// A block of threads owns kP x kQ entries of D, its waves TP x TQ accumulators of 32 x 32 each.  K-tiles are 128 bytes of every row of both
+// operands, which come by direct global->LDS loads, across the ends of tiles: a block takes tile after tile as one sequence of K-tiles.
+// In LDS each operand has a ring of its own, NP and NQ K-tiles long.  The widest form, four waves of 128 x 128, has room for 3 + 2 and nothing else; its results
+// turn into rows in the slot of P that waits for its loads.
+// What bounds it: the matrix cores run at the chip's power limit (1.8 GHz of 2.4), and beside them the loads.  Rows in pieces of 64 bytes, half a
+// cache line, come at 10 TB/s over the chip and no more: 64-byte K-tiles in a ring of four took 0.82 us a K-tile of the widest form, the same
+// bytes as whole lines 0.70, no loads at all 0.63.  A wave of 128 x 128 leaves one wave to a SIMD, so its fragments are read
+// behind the products of the step before.
 //
 // In the accumulators of a 32 x 32 product a lane holds one column (q) and four consecutive rows (p) at a time, so D goes to memory as [q][p]:
 // P is the operand whose rows are contiguous in the result.
@@ -24,34 +26,39 @@ namespace cdl {
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 
-constexpr int kRingRow = 64;      // bytes of a row in a K-tile
+constexpr int kRingRow = 128;      // bytes of a row in a K-tile
 // s_waitcnt of loads (and stores) still under way, and of all LDS reads
 constexpr int wait_imm(int vm) { return (vm & 15) | ((vm >> 4) << 14) | 0x0070; }
 
-// WP x WQ waves of TP x TQ accumulators; STAGING: LDS bytes in which a wave turns its results into rows; SCALES: a byte for every row comes with a K-tile
-template <int WP_, int WQ_, int TP_, int TQ_, int RING_, int PER_CU_, int STAGING_, bool SCALES_ = false>
+// WP x WQ waves of TP x TQ accumulators; NP, NQ: K-tiles of each operand in LDS; STAGING: LDS bytes in which a wave turns its results into rows, 0: in the slot of P
+// that is free then; SCALES: a byte for every row comes with a K-tile.
+// After a K-tile its slots are free.  The loads of Q into its slot go out with the last products of the K-tile, those of P with the first ones of the next K-tile
+// (behind a tile's results), or with those of Q where P has no third slot.
+template <int WP_, int WQ_, int TP_, int TQ_, int NP_, int NQ_, int PER_CU_, int STAGING_ = 0, bool SCALES_ = false>
 struct RingForm {
-    static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, RING = RING_, PER_CU = PER_CU_, STAGING = STAGING_;
-    static constexpr bool SCALES = SCALES_;
+    static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, NP = NP_, NQ = NQ_, PER_CU = PER_CU_;
+    static constexpr bool SCALES = SCALES_, kTogether = NP == 2;
     static constexpr int kWaves = WP * WQ, kThreads = 64 * kWaves, kP = WP * TP * 32, kQ = WQ * TQ * 32;
-    static constexpr int kOperands = (kP + kQ) * kRingRow, kScaleBytes = 256, kStage = kOperands + (SCALES ? 2 * kScaleBytes : 0);
-    static constexpr int kLds = RING * kStage + kWaves * STAGING;
-    static constexpr int kLoadsP = kP / 16 / kWaves, kLoadsQ = kQ / 16 / kWaves, kLoads = kLoadsP + kLoadsQ + (SCALES ? 1 : 0);      // of a wave and K-tile
-    static_assert(kLoadsP * 16 * kWaves == kP && kLoadsQ * 16 * kWaves == kQ && RING >= 3, "whole loads of 1 KB; a stage free while the next is read");
+    static constexpr int kSlotP = kP * kRingRow, kSlotQ = kQ * kRingRow, kScaleBytes = 256, kSlotS = SCALES ? 2 * kScaleBytes : 0;
+    static constexpr int kAtQ = NP * kSlotP, kAtS = kAtQ + NQ * kSlotQ, kAtStaging = kAtS + NQ * kSlotS, kLds = kAtStaging + kWaves * STAGING_;
+    static constexpr int kLoadsP = kP / 8 / kWaves, kLoadsQ = kQ / 8 / kWaves, kMoreQ = kLoadsQ + (SCALES ? 1 : 0);      // of a wave and K-tile, 1 KB each; and the scales
+    static constexpr int STAGING = STAGING_ ? STAGING_ : kLoadsP * 1024;
+    static_assert(kLoadsP * 8 * kWaves == kP && kLoadsQ * 8 * kWaves == kQ && (NP == NQ || NP == NQ + 1) && NQ >= 2, "whole loads; the order of the loads");
+    static_assert(!kTogether || STAGING_ > 0, "a free slot of P between tiles");
     static_assert(PER_CU * kLds <= 160 << 10 && kP <= 256 && kQ <= 256 && kWaves % 2 == 0, "LDS; scales of an operand in one load");
 };
 
 struct RingJob {
-    const uint8_t *P, *Q;          // 16-byte aligned, rows ldp, ldq bytes apart (multiples of 16, 256 of them within 4 GiB)
+    const uint8_t *P, *Q;          // 16-byte aligned, rows ldp, ldq bytes apart (multiples of 16, 256 of them within 4 GiB - 8 KiB)
     int64_t ldp, ldq;
     int rowsP, rowsQ;
-    int nk;                        // K-tiles in all, even
+    int nk;                        // K-tiles in all
     int tiles_p, tiles_q;
-    int splits, k_per;             // the contraction in `splits` parts of k_per K-tiles (even; the last may be shorter, none is empty)
+    int splits, k_per;             // the contraction in `splits` parts of k_per K-tiles (the last may be shorter, none is empty)
     // an operand in three parts: their products one after the other, plane_nk K-tiles each, parts plane_p and plane_q bytes apart
     int plane_nk;
     int64_t plane_p, plane_q;
-    const uint8_t *sp, *sq;        // scales: [128 bytes of K][pitch], pitches multiples of 128
+    const uint8_t *sp, *sq;        // scales: [K-tile][pitch], pitches multiples of 128
     int64_t pitch_sp, pitch_sq;
 };
 
@@ -67,7 +74,8 @@ __device__ __forceinline__ RingUnit ring_unit(const RingJob &job, int unit)
 }
 
 struct OpBf16 {
-    static constexpr int KS = 2;      // steps of a K-tile
+    static constexpr bool kPin = false;
+    static constexpr int KS = 4, kReads = 1, kPerPair = 1, kConversions = 0;      // steps of a K-tile; reads of a fragment, instructions of a product, conversions beside each
     typedef bf16x8 Frag;
     static __device__ __forceinline__ Frag read(const uint8_t *row, const int *chunk, int ks)
     {
@@ -94,11 +102,12 @@ struct OpBf16 {
 // the bf16 instruction, whose products and sums are those of fp32, at half the rate.
 template <int FP, int FQ, bool EXACT>
 struct OpF8 {
-    static constexpr int KS = 1;
+    static constexpr bool kPin = true;
+    static constexpr int KS = 2, kReads = 2, kPerPair = EXACT ? 4 : 1, kConversions = EXACT ? 2 : 0;
     typedef v8i Frag;
-    static __device__ __forceinline__ Frag read(const uint8_t *row, const int *chunk, int)
+    static __device__ __forceinline__ Frag read(const uint8_t *row, const int *chunk, int ks)
     {
-        const v4i a = *reinterpret_cast<const v4i *>(row + chunk[0]), b = *reinterpret_cast<const v4i *>(row + chunk[1]);
+        const v4i a = *reinterpret_cast<const v4i *>(row + chunk[2 * ks]), b = *reinterpret_cast<const v4i *>(row + chunk[2 * ks + 1]);
         return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     template <int F>
@@ -140,78 +149,94 @@ struct OpF8 {
     }
 };
 
-// Where a wave's loads come from.
-template <class FORM, bool PLANES>
-struct RingSource {
-    const RingJob &job;
-    int unit, last, each, kt, end, in_plane, product;
-    const uint8_t *src_p, *src_q, *src_s;
-    uint32_t off_p[FORM::kLoadsP], off_q[FORM::kLoadsQ], off_s;
+// Where the loads of an operand come from: K-tile after K-tile, `left` of them before change() has to be called, which goes on to the next unit of work (or to
+// the next product of parts).  Four loads share a base in LDS: the instruction's offset counts on both sides, so a lane's offset into memory
+// takes it back.
+template <class FORM, bool PLANES, bool IS_P>
+struct RingStream {
+    static constexpr int kLoads = IS_P ? FORM::kLoadsP : FORM::kLoadsQ, kBack = 4096;      // (offsets stay positive)
+    int unit, left, end, product;
+    const uint8_t *src, *src_s;
+    uint32_t off[kLoads], off_s;
     int64_t step_s;
 
     // parts multiplied, of P and of Q: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
-    static __device__ __forceinline__ int part_p(int product) { return (0x850 >> (2 * product)) & 3; }
-    static __device__ __forceinline__ int part_q(int product) { return (0x244 >> (2 * product)) & 3; }
+    static __device__ __forceinline__ int part(int product) { return ((IS_P ? 0x850 : 0x244) >> (2 * product)) & 3; }
 
-    __device__ __forceinline__ void start(int wave, int lane)
+    __device__ __forceinline__ void start(const RingJob &job, int wave, int lane)
     {
         const RingUnit u = ring_unit<FORM>(job, unit);
-        kt = u.split * job.k_per;
+        const int kt = u.split * job.k_per, row0 = IS_P ? u.p0 : u.q0, rows = IS_P ? job.rowsP : job.rowsQ;
+        const int64_t ld = IS_P ? job.ldp : job.ldq;
         end = min(kt + job.k_per, job.nk);
         product = PLANES ? kt / job.plane_nk : 0;
-        in_plane = PLANES ? kt - product * job.plane_nk : kt;
-        src_p = job.P + (int64_t)u.p0 * job.ldp + (int64_t)in_plane * kRingRow + (PLANES ? part_p(product) * job.plane_p : 0);
-        src_q = job.Q + (int64_t)u.q0 * job.ldq + (int64_t)in_plane * kRingRow + (PLANES ? part_q(product) * job.plane_q : 0);
-        const uint32_t chunk = (uint32_t)(((lane & 3) ^ ((lane >> 4) & 3)) * 16);
+        const int in_plane = PLANES ? kt - product * job.plane_nk : kt;
+        left = PLANES ? min(job.plane_nk - in_plane, end - kt) : end - kt;
+        src = (IS_P ? job.P : job.Q) + (int64_t)row0 * ld + (int64_t)in_plane * kRingRow + (PLANES ? part(product) * (IS_P ? job.plane_p : job.plane_q) : 0) - kBack;
 #pragma unroll
-        for (int i = 0; i < FORM::kLoadsP; ++i)      // (rows beyond the matrix: its last one again, whose results nobody stores)
-            off_p[i] = (uint32_t)min((wave * FORM::kLoadsP + i) * 16 + (lane >> 2), job.rowsP - 1 - u.p0) * (uint32_t)job.ldp + chunk;
-#pragma unroll
-        for (int i = 0; i < FORM::kLoadsQ; ++i)
-            off_q[i] = (uint32_t)min((wave * FORM::kLoadsQ + i) * 16 + (lane >> 2), job.rowsQ - 1 - u.q0) * (uint32_t)job.ldq + chunk;
-        if (FORM::SCALES) {      // four bytes a lane; half of the waves load those of P, the others those of Q
+        for (int i = 0; i < kLoads; ++i) {      // load i fills LDS rows 8 n ... 8 n + 7, chunk c of a row at c ^ (row / 2); rows beyond the matrix: its last one again, whose results nobody stores
+            const int n = wave * kLoads + i;
+            off[i] = (uint32_t)min(n * 8 + (lane >> 3), rows - 1 - row0) * (uint32_t)ld + (uint32_t)((lane & 7) ^ ((4 * n + (lane >> 4)) & 7)) * 16 + kBack - (i & 3) * 1024;
+        }
+        if (FORM::SCALES && !IS_P) {      // four bytes a lane; half of the waves load those of Q, the others those of P
             const bool q = wave & 1;
             const int64_t pitch = q ? job.pitch_sq : job.pitch_sp;
             const int at = q ? u.q0 : u.p0;
-            src_s = (q ? job.sq : job.sp) + at + (int64_t)(kt >> 1) * pitch;
+            src_s = (q ? job.sq : job.sp) + at + (int64_t)kt * pitch;
             off_s = (uint32_t)min((int64_t)lane * 4, pitch - 4 - at);
             step_s = pitch;
         }
     }
-    __device__ __forceinline__ void issue(uint8_t *stage, int wave, int lane)
+    __device__ __forceinline__ void change(const RingJob &job, int each, int last, int wave, int lane)
     {
-        uint8_t *const to_p = stage + wave * FORM::kLoadsP * 1024, *const to_q = stage + FORM::kP * kRingRow + wave * FORM::kLoadsQ * 1024;
-#pragma unroll
-        for (int i = 0; i < FORM::kLoadsP; ++i) __builtin_amdgcn_global_load_lds((gptr_t)(src_p + off_p[i]), (lptr_t)(to_p + i * 1024), 16, 0, 0);
-#pragma unroll
-        for (int i = 0; i < FORM::kLoadsQ; ++i) __builtin_amdgcn_global_load_lds((gptr_t)(src_q + off_q[i]), (lptr_t)(to_q + i * 1024), 16, 0, 0);
-        if (FORM::SCALES) {
-            __builtin_amdgcn_global_load_lds((gptr_t)(src_s + off_s), (lptr_t)(stage + FORM::kOperands + (wave & 1) * FORM::kScaleBytes), 4, 0, 0);
-            if (kt & 1) src_s += step_s;      // (one scale for 128 bytes of a row: two K-tiles)
-        }
-        src_p += kRingRow;
-        src_q += kRingRow;
-        ++kt;
-        if (PLANES && ++in_plane == job.plane_nk) {
-            in_plane = 0;
-            ++product;
-            if (kt < end) {
-                src_p += (part_p(product) - part_p(product - 1)) * job.plane_p - (int64_t)job.plane_nk * kRingRow;
-                src_q += (part_q(product) - part_q(product - 1)) * job.plane_q - (int64_t)job.plane_nk * kRingRow;
+        if (PLANES) {
+            const int next = (product + 1) * job.plane_nk;
+            if (next < end) {
+                ++product;
+                src += (part(product) - part(product - 1)) * (IS_P ? job.plane_p : job.plane_q) - (int64_t)job.plane_nk * kRingRow;
+                left = min(job.plane_nk, end - next);
+                return;
             }
         }
-        if (kt == end) {
-            unit = min(unit + each, last);      // (past the last unit: the last one again, which nobody reads)
-            start(wave, lane);
+        unit = min(unit + each, last);      // (past the last unit: the last one again, which nobody reads)
+        start(job, wave, lane);
+    }
+    // loads FROM .. TO - 1 of a K-tile
+    template <int FROM, int TO>
+    __device__ __forceinline__ void issue(uint8_t *slot, int wave) const
+    {
+        if constexpr (FROM < TO) {
+            __builtin_amdgcn_global_load_lds((gptr_t)(src + off[FROM]), (lptr_t)(slot + wave * kLoads * 1024 + (FROM & ~3) * 1024), 16, (FROM & 3) * 1024, 0);
+            issue<FROM + 1, TO>(slot, wave);
         }
+    }
+    __device__ __forceinline__ void issue_scales(uint8_t *slot, int wave)
+    {
+        __builtin_amdgcn_global_load_lds((gptr_t)(src_s + off_s), (lptr_t)(slot + (wave & 1) * FORM::kScaleBytes), 4, 0, 0);
+        src_s += step_s;
     }
 };
 
-// epilogue(acc, p0, q0, split): first entries of the wave's part of a tile; stores at least EPILOGUE::kStores times for a wave or waits for its stores.
+// The order of instructions that the loop asks for: reads behind the first products, so that they have come by the next step, loads evenly.
+template <int I, int PRODUCTS, int READS, int LOADS, int CONVERSIONS>
+__device__ __forceinline__ void mix_slots()
+{
+    if constexpr (I < PRODUCTS) {
+        constexpr int kHalf = PRODUCTS / 2 > 0 ? PRODUCTS / 2 : 1, kReads = I < kHalf ? (I + 1) * READS / kHalf - I * READS / kHalf : 0;
+        constexpr int kLoads = (I + 1) * LOADS / PRODUCTS - I * LOADS / PRODUCTS;
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if constexpr (CONVERSIONS > 0) __builtin_amdgcn_sched_group_barrier(0x002, CONVERSIONS, 0);
+        if constexpr (kReads > 0) __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+        if constexpr (kLoads > 0) __builtin_amdgcn_sched_group_barrier(0x010, kLoads, 0);
+        mix_slots<I + 1, PRODUCTS, READS, LOADS, CONVERSIONS>();
+    }
+}
+
+// epilogue(acc, p0, q0, split, staging, lane): first entries of the wave's part of a tile; stores at least EPILOGUE::kStores times for a wave or waits for its stores.
 template <class FORM, class OP, bool PLANES, class EPILOGUE>
 __device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
 {
-    constexpr int TP = FORM::TP, TQ = FORM::TQ, AHEAD = FORM::RING - 1, KS = OP::KS;
+    constexpr int TP = FORM::TP, TQ = FORM::TQ, KS = OP::KS;
     extern __shared__ __attribute__((aligned(16))) uint8_t ring_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wp = wave / FORM::WQ, wq = wave % FORM::WQ;
@@ -221,31 +246,34 @@ __device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
     const int first = xcd * share + ((int)blockIdx.x >> 3), end = min(total, (xcd + 1) * share);
     if (first >= end) return;
 
-    RingSource<FORM, PLANES> source{job};
-    source.unit = first;
-    source.each = each;
-    source.last = total - 1;
-    source.start(wave, lane);
+    RingStream<FORM, PLANES, true> from_p;
+    RingStream<FORM, PLANES, false> from_q;
+    from_p.unit = from_q.unit = first;
+    from_p.start(job, wave, lane);
+    from_q.start(job, wave, lane);
 
-    const int row = lane & 31, half = lane >> 5, swz = (row >> 2) & 3;
-    const int chunk[2] = {row * kRingRow + (half ^ swz) * 16, row * kRingRow + ((2 + half) ^ swz) * 16};
-    const int at_p = wp * TP * 32 * kRingRow, at_q = (FORM::kP + wq * TQ * 32) * kRingRow;
+    const int row = lane & 31, half = lane >> 5;
+    int chunk[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) chunk[c] = row * kRingRow + (((2 * c + half) ^ (row >> 1)) & 7) * 16;
 
     v16f acc[TP][TQ];
     typename OP::Frag fp[2][TP], fq[2][TQ];
     int sp[2][TP], sq[2][TQ];
-    auto read = [&](int stage, int ks, auto set_c) {
+    int at_p = 0, at_q = 0, at_s = 0;      // of the K-tile being multiplied: its slots
+    auto read = [&](int ks, auto set_c) {
         constexpr int S = decltype(set_c)::value;
-        const uint8_t *const base = ring_lds + stage * FORM::kStage;
+        const uint8_t *const p = ring_lds + at_p + wp * TP * 32 * kRingRow, *const q = ring_lds + FORM::kAtQ + at_q + wq * TQ * 32 * kRingRow;
 #pragma unroll
-        for (int i = 0; i < TP; ++i) fp[S][i] = OP::read(base + at_p + i * 32 * kRingRow, chunk, ks);
+        for (int i = 0; i < TP; ++i) fp[S][i] = OP::read(p + i * 32 * kRingRow, chunk, ks);
 #pragma unroll
-        for (int j = 0; j < TQ; ++j) fq[S][j] = OP::read(base + at_q + j * 32 * kRingRow, chunk, ks);
+        for (int j = 0; j < TQ; ++j) fq[S][j] = OP::read(q + j * 32 * kRingRow, chunk, ks);
         if (FORM::SCALES) {
+            const uint8_t *const scales = ring_lds + FORM::kAtS + at_s;
 #pragma unroll
-            for (int i = 0; i < TP; ++i) sp[S][i] = base[FORM::kOperands + (wp * TP + i) * 32 + row];
+            for (int i = 0; i < TP; ++i) sp[S][i] = scales[(wp * TP + i) * 32 + row];
 #pragma unroll
-            for (int j = 0; j < TQ; ++j) sq[S][j] = base[FORM::kOperands + FORM::kScaleBytes + (wq * TQ + j) * 32 + row];
+            for (int j = 0; j < TQ; ++j) sq[S][j] = scales[FORM::kScaleBytes + (wq * TQ + j) * 32 + row];
         }
     };
     auto multiply = [&](auto set_c, auto first_c) {
@@ -254,59 +282,110 @@ __device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
     };
     typedef std::integral_constant<int, 0> Zero;
     typedef std::integral_constant<int, 1> One;
+    typedef std::true_type Yes;
+    typedef std::false_type No;
 
-    int stage = 0, since = 1 << 20;      // K-tiles since a tile's stores
-    // The loads of the next K-tile have landed - younger are those of RING - 3 K-tiles, and, where they were asked for before the stores of the last tile, at least
-    // those: loads and stores are counted together, up to 63, in order -, this wave has its fragments, and every wave has left the stage before.
-    auto turn = [&]() {
-        constexpr int kLoads = (FORM::RING - 3) * FORM::kLoads, kBoth = kLoads + EPILOGUE::kStores < 63 ? kLoads + EPILOGUE::kStores : 63;
-        if (since < FORM::RING - 2) __builtin_amdgcn_s_waitcnt(wait_imm(kBoth));
-        else __builtin_amdgcn_s_waitcnt(wait_imm(kLoads));
-        ++since;
+    int free_p = 0, free_q = 0, free_s = 0;      // the slots that the next loads fill
+    auto loaded_p = [&]() {
+        free_p = free_p == (FORM::NP - 1) * FORM::kSlotP ? 0 : free_p + FORM::kSlotP;
+        from_p.src += kRingRow;
+        __builtin_amdgcn_sched_barrier(0);
+        if (--from_p.left == 0) from_p.change(job, each, total - 1, wave, lane);
+    };
+    auto issue_q = [&]() {
+        from_q.template issue<0, FORM::kLoadsQ>(ring_lds + FORM::kAtQ + free_q, wave);
+        if (FORM::SCALES) from_q.issue_scales(ring_lds + FORM::kAtS + free_s, wave);
+    };
+    auto loaded_q = [&]() {
+        free_q = free_q == (FORM::NQ - 1) * FORM::kSlotQ ? 0 : free_q + FORM::kSlotQ;
+        if (FORM::SCALES) free_s = free_s == (FORM::NQ - 1) * FORM::kSlotS ? 0 : free_s + FORM::kSlotS;
+        from_q.src += kRingRow;
+        __builtin_amdgcn_sched_barrier(0);
+        if (--from_q.left == 0) from_q.change(job, each, total - 1, wave, lane);
+    };
+    auto barrier = [&]() {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        source.issue(ring_lds + (stage == 0 ? FORM::RING - 1 : stage - 1) * FORM::kStage, wave, lane);
-        stage = stage + 1 == FORM::RING ? 0 : stage + 1;
     };
-    auto pair = [&](auto first_c) {      // two K-tiles
+    // The loads of the next K-tile have landed - younger are those of NQ - 2 whole K-tiles and of one more of P where it has a slot more, and for the first K-tile of a
+    // tile the stores of the tile before, at least: loads and stores are counted together, up to 63, in order -, this wave has its fragments, and every
+    // wave has read what it needs of the K-tile.
+    bool stored = false;
+    auto turn = [&](auto early_c) {
+        constexpr int kYounger = (FORM::NQ - 2) * (FORM::kLoadsP + FORM::kMoreQ) + (FORM::NP > FORM::NQ ? FORM::kLoadsP : 0);
+        constexpr int kBoth = kYounger + EPILOGUE::kStores < 63 ? kYounger + EPILOGUE::kStores : 63;
+        static_assert(kYounger < 64, "loads that the counter holds");
+        __builtin_amdgcn_sched_barrier(0);
+        if (decltype(early_c)::value && stored) __builtin_amdgcn_s_waitcnt(wait_imm(kBoth));
+        else __builtin_amdgcn_s_waitcnt(wait_imm(kYounger));
+        barrier();
+    };
+    // Nothing else fills a SIMD's matrix cores while its only wave reads or loads, so reads and loads go between the products, and the products of a step stay on their side
+    // of the barrier (left to itself the compiler gathers the reads before the wait and the products behind it).
+    constexpr int kFragments = (TP + TQ) * OP::kReads + (FORM::SCALES ? TP + TQ : 0), kProducts = TP * TQ * OP::kPerPair;
+    auto step = [&](auto first_c) {      // a K-tile, the first one of a tile or a later one
         typedef decltype(first_c) First;
-        if constexpr (KS == 2) {
-            read(stage, 1, One{});
-            multiply(Zero{}, First{});
-            turn();
-            read(stage, 0, Zero{});
-            multiply(One{}, std::false_type{});
-            read(stage, 1, One{});
-            multiply(Zero{}, std::false_type{});
-            turn();
-            read(stage, 0, Zero{});
-            multiply(One{}, std::false_type{});
-        } else {
-            turn();
-            read(stage, 0, One{});
-            multiply(Zero{}, First{});
-            turn();
-            read(stage, 0, Zero{});
-            multiply(One{}, std::false_type{});
+        auto inner = [&](auto r_c) {
+            constexpr int R = decltype(r_c)::value, kFrom = FORM::kTogether ? 0 : FORM::kLoadsP * R / (KS - 1), kTo = FORM::kTogether ? 0 : FORM::kLoadsP * (R + 1) / (KS - 1);
+            read(R + 1, std::integral_constant<int, (R + 1) & 1>{});
+            from_p.template issue<kFrom, kTo>(ring_lds + free_p, wave);
+            multiply(std::integral_constant<int, R & 1>{}, std::integral_constant<bool, First::value && R == 0>{});
+            mix_slots<0, kProducts, kFragments, kTo - kFrom, OP::kConversions>();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        inner(Zero{});
+        if constexpr (KS == 4) {
+            inner(One{});
+            inner(std::integral_constant<int, 2>{});
         }
+        if constexpr (!FORM::kTogether) loaded_p();
+        turn(First{});
+        at_p = at_p == (FORM::NP - 1) * FORM::kSlotP ? 0 : at_p + FORM::kSlotP;
+        at_q = at_q == (FORM::NQ - 1) * FORM::kSlotQ ? 0 : at_q + FORM::kSlotQ;
+        if (FORM::SCALES) at_s = at_s == (FORM::NQ - 1) * FORM::kSlotS ? 0 : at_s + FORM::kSlotS;
+        read(0, Zero{});
+        issue_q();
+        if constexpr (FORM::kTogether) from_p.template issue<0, FORM::kLoadsP>(ring_lds + free_p, wave);
+        multiply(One{}, No{});
+        mix_slots<0, kProducts, kFragments, FORM::kMoreQ + (FORM::kTogether ? FORM::kLoadsP : 0), OP::kConversions>();
+        if constexpr (OP::kPin) {      // (a use of the products on this side of the branch below: the compiler would move them behind it, away from the reads and loads)
+#pragma unroll
+            for (int i = 0; i < TP; ++i)
+#pragma unroll
+                for (int j = 0; j < TQ; ++j) asm volatile("" ::"a"(acc[i][j]));
+        }
+        loaded_q();
+        if constexpr (FORM::kTogether) loaded_p();
     };
 
-    for (int s = 0; s < AHEAD; ++s) source.issue(ring_lds + s * FORM::kStage, wave, lane);
-    __builtin_amdgcn_s_waitcnt(wait_imm((AHEAD - 1) * FORM::kLoads));
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    read(0, 0, Zero{});
+    // the order that the loop keeps: Q of a K-tile, then P of that K-tile, or of the next one where P has a slot more; the last one of P comes with the first step
+#pragma unroll
+    for (int k = FORM::NQ - FORM::NP; k < FORM::NQ; ++k) {
+        if (k >= 0) {
+            issue_q();
+            loaded_q();
+        }
+        if (k < FORM::NQ - 1 || FORM::kTogether) {
+            from_p.template issue<0, FORM::kLoadsP>(ring_lds + free_p, wave);
+            loaded_p();
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(wait_imm((FORM::NP - (FORM::kTogether ? 1 : 2)) * FORM::kLoadsP + (FORM::NQ - 1) * FORM::kMoreQ));
+    barrier();
+    read(0, Zero{});
     for (int unit = first; unit < end; unit += each) {
         const RingUnit u = ring_unit<FORM>(job, unit);
-        const int pairs = (min(job.k_per, job.nk - u.split * job.k_per)) >> 1;
-        pair(std::true_type{});
-        for (int k = 1; k < pairs; ++k) pair(std::false_type{});
+        const int count = min(job.k_per, job.nk - u.split * job.k_per);
+        step(Yes{});
+        for (int k = 1; k < count; ++k) step(No{});
         int own = lane;
         asm volatile("" : "+v"(own));      // (what the results' places are made of is formed here, not held through the loop)
-        epilogue(acc, u.p0 + wp * TP * 32, u.q0 + wq * TQ * 32, u.split, ring_lds + FORM::RING * FORM::kStage + wave * FORM::STAGING, own);
-        since = 0;
+        // the wave's own part of the free slot of P, which its own next loads fill; every wave has left that K-tile
+        uint8_t *const staging = ring_lds + (FORM::kTogether || FORM::kLds > FORM::kAtStaging ? FORM::kAtStaging + wave * FORM::STAGING : free_p + wave * FORM::kLoadsP * 1024);
+        epilogue(acc, u.p0 + wp * TP * 32, u.q0 + wq * TQ * 32, u.split, staging, own);
+        stored = true;
+        read(0, Zero{});      // (again: the fragments would take registers that the results need)
     }
     __builtin_amdgcn_s_waitcnt(wait_imm(0));      // the loads behind the last step write LDS: done before this wave ends
 }

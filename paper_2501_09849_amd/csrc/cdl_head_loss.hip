@@ -25,7 +25,7 @@ __device__ __forceinline__ void find_target(const v16f (&acc)[FORM::TP][FORM::TQ
 #pragma unroll
     for (int i = 0; i < FORM::TP; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) z = i * 32 + 8 * (r >> 2) + (r & 3) == own ? acc[i][j][r] : z;
+        for (int r = 0; r < 16; ++r) z = i * 32 + 8 * (r >> 2) + (r & 3) == own ? result<FORM>(acc[i][j], r) : z;
     *(here ? to : spare) = f(z);
 }
 
@@ -52,7 +52,7 @@ struct Reduce {
 #pragma unroll
         for (int j = 0; j < TQ; ++j) {
             float m = -INFINITY, s = 0.0f;
-            auto value = [&](int i, int r) { return FULL || i * 32 + 8 * (r >> 2) + (r & 3) < left ? acc[i][j][r] : -INFINITY; };
+            auto value = [&](int i, int r) { return FULL || i * 32 + 8 * (r >> 2) + (r & 3) < left ? result<FORM>(acc[i][j], r) : -INFINITY; };
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
@@ -348,6 +348,9 @@ Form choose_form(int64_t rows_p, int64_t rows_q)
 
 int64_t up(int64_t n, int64_t by) { return (n + by - 1) / by * by; }
 
+// Pitch of rows of n entries (a multiple of 64) in the workspace: an odd number of cache lines, so that the rows of a tile do not start in the same memory channel.
+int64_t line_pitch(int64_t n) { return n / 64 % 2 ? n : n + 64; }
+
 struct Split { int splits, k_per; };
 Split choose_splits(int64_t tiles, int per_cu, int nk)
 {
@@ -363,12 +366,12 @@ constexpr int64_t kPieceEntries = 1 << 27;
 
 struct Plan {
     int parts;
-    int64_t Dp, Tp;                   // up to multiples of 64
+    int64_t Dp, Tp, Tl;               // up to multiples of 64; pitch of rows of tokens
     bool copy;                        // the operands as rows of Dp entries in the workspace
     Form reduce;
     int64_t stretches;
     // training
-    int64_t piece, piece_p;           // entries of the vocabulary at a time, up to a multiple of 64
+    int64_t piece, piece_l;           // entries of the vocabulary at a time; pitch of their rows
     Form gradient, form_h, form_w;
     Split split_h;
     int64_t tokens;                   // of the table, whole tiles
@@ -382,6 +385,7 @@ Plan make_plan(int64_t T, int64_t V, int64_t D, int32_t type, bool train)
     p.parts = type == CDL_F32 ? 3 : 1;
     p.Dp = D == 0 ? 64 : up(D, 64);
     p.Tp = up(T, 64);
+    p.Tl = line_pitch(p.Tp);
     p.copy = type == CDL_F32 || p.Dp != D;
     p.reduce = choose_form(V, T);
     p.stretches = (V + form_stretch(p.reduce) - 1) / form_stretch(p.reduce);
@@ -404,16 +408,16 @@ Plan make_plan(int64_t T, int64_t V, int64_t D, int32_t type, bool train)
         most = most < 2048 ? 2048 : most > 1 << 22 ? 1 << 22 : most;      // (256 rows of g transposed within 32-bit offsets)
         const int64_t pieces = (V + most - 1) / most;
         p.piece = pieces == 1 ? V : up((V + pieces - 1) / pieces, 256);
-        p.piece_p = up(p.piece, 64);
+        p.piece_l = line_pitch(up(p.piece, 64));
         p.gradient = choose_form(p.piece, T);
         p.form_h = choose_form(D, T);
         p.form_w = choose_form(D, p.piece);
         const int64_t tiles = ((D + form_p(p.form_h) - 1) / form_p(p.form_h)) * ((T + form_q(p.form_h) - 1) / form_q(p.form_h));
-        p.split_h = choose_splits(tiles < 1 ? 1 : tiles, form_per_cu(p.form_h), (int)(p.piece_p / 64 * (p.parts == 3 ? 6 : 1)));
-        p.ht = take(p.parts * up(D, 64) * p.Tp * 2);
-        p.wt = take(p.parts * up(D, 64) * p.piece_p * 2);
-        p.g = take(p.parts * T * p.piece_p * 2);
-        p.gt = take(p.parts * p.piece_p * p.Tp * 2);
+        p.split_h = choose_splits(tiles < 1 ? 1 : tiles, form_per_cu(p.form_h), (int)(up(p.piece, 64) / 64 * (p.parts == 3 ? 6 : 1)));
+        p.ht = take(p.parts * up(D, 64) * p.Tl * 2);
+        p.wt = take(p.parts * up(D, 64) * p.piece_l * 2);
+        p.g = take(p.parts * T * p.piece_l * 2);
+        p.gt = take(p.parts * p.piece_l * p.Tl * 2);
         p.sums = take((int64_t)p.split_h.splits * T * D * 4);
         if (at < forward) at = forward;
     }
@@ -540,21 +544,21 @@ int backward(const T *h, const T *w, int32_t type, const int64_t *target, const 
                (const float *)unit, table);
     CDL_TRY(check_launch());
     bf16_t *const ht = (bf16_t *)(ws + p.ht), *const wt = (bf16_t *)(ws + p.wt), *const g = (bf16_t *)(ws + p.g), *const gt = (bf16_t *)(ws + p.gt);
-    if (d_w) CDL_TRY(transpose(ph, p.Dp, tokens * p.Dp, tokens, D, ht, p.Tp, up(D, 64) * p.Tp, p.parts, stream));
-    const int64_t plane_g = tokens * p.piece_p;
+    if (d_w) CDL_TRY(transpose(ph, p.Dp, tokens * p.Dp, tokens, D, ht, p.Tl, up(D, 64) * p.Tl, p.parts, stream));
+    const int64_t plane_g = tokens * p.piece_l;
     for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
         const int64_t cols = v0 + p.piece <= V ? p.piece : V - v0, padded = up(cols, 64);
         const bf16_t *const piece = pw + v0 * p.Dp;
         {
             const RingJob job = ring_job(p.gradient, piece, p.Dp, cols, ph, p.Dp, tokens, p.Dp, p.parts, V * p.Dp, tokens * p.Dp);
-            CDL_TRY(run_gradient<PARTS>(p, job, RowTarget<bf16_t>{g, p.piece_p, (int)padded, tokens, 16}, table, at_target, tokens, (int)v0, (int)cols, plane_g, stream));
-            CDL_LAUNCH("head_target_kernel", stream, head_target_kernel, dim3(blocks_of(tokens, 256)), dim3(256), 0, (const Token *)table, (const float *)at_target, tokens, (int)v0, (int)cols, g, p.piece_p,
+            CDL_TRY(run_gradient<PARTS>(p, job, RowTarget<bf16_t>{g, p.piece_l, (int)padded, tokens, 16}, table, at_target, tokens, (int)v0, (int)cols, plane_g, stream));
+            CDL_LAUNCH("head_target_kernel", stream, head_target_kernel, dim3(blocks_of(tokens, 256)), dim3(256), 0, (const Token *)table, (const float *)at_target, tokens, (int)v0, (int)cols, g, p.piece_l,
                        plane_g, p.parts);
             CDL_TRY(check_launch());
         }
         if (d_h) {
-            CDL_TRY(transpose(piece, p.Dp, V * p.Dp, cols, D, wt, p.piece_p, up(D, 64) * p.piece_p, p.parts, stream));
-            RingJob job = ring_job(p.form_h, wt, p.piece_p, D, g, p.piece_p, tokens, padded, p.parts, up(D, 64) * p.piece_p, plane_g);
+            CDL_TRY(transpose(piece, p.Dp, V * p.Dp, cols, D, wt, p.piece_l, up(D, 64) * p.piece_l, p.parts, stream));
+            RingJob job = ring_job(p.form_h, wt, p.piece_l, D, g, p.piece_l, tokens, padded, p.parts, up(D, 64) * p.piece_l, plane_g);
             job.k_per = p.split_h.k_per;
             job.splits = (job.nk + job.k_per - 1) / job.k_per;      // (a last, shorter piece: fewer parts)
             const RowTarget<float> to{sums, D, D, tokens, row_width(sums, (int64_t)D * 4)};
@@ -562,8 +566,8 @@ int backward(const T *h, const T *w, int32_t type, const int64_t *target, const 
             CDL_TRY(v0 == 0 ? (run_product<PARTS, float, false>(p.form_h, job, to, part, nullptr, stream)) : (run_product<PARTS, float, true>(p.form_h, job, to, part, nullptr, stream)));
         }
         if (d_w) {
-            CDL_TRY(transpose(g, p.piece_p, plane_g, tokens, cols, gt, p.Tp, p.piece_p * p.Tp, p.parts, stream));
-            const RingJob job = ring_job(p.form_w, ht, p.Tp, D, gt, p.Tp, cols, p.Tp, p.parts, up(D, 64) * p.Tp, p.piece_p * p.Tp);
+            CDL_TRY(transpose(g, p.piece_l, plane_g, tokens, cols, gt, p.Tl, p.piece_l * p.Tl, p.parts, stream));
+            const RingJob job = ring_job(p.form_w, ht, p.Tl, D, gt, p.Tl, cols, p.Tp, p.parts, up(D, 64) * p.Tl, p.piece_l * p.Tl);
             T *const out = d_w + v0 * D;
             CDL_TRY((run_product<PARTS, T, false>(p.form_w, job, RowTarget<T>{out, D, D, (int)cols, row_width(out, (int64_t)D * (int64_t)sizeof(T))}, 0, unit, stream)));
         }

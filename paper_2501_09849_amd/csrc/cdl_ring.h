@@ -232,6 +232,30 @@ __device__ __forceinline__ void mix_slots()
     }
 }
 
+// The accumulators of the widest form fill the half of the registers that only the matrix cores and moves reach.  The results are moved out one at a time, where they are
+// used: left to itself the compiler moves whole accumulators, spills what there was, and every reload waits for the stores before it (an epilogue of
+// 128 x 128 results a wave took 20 to 50 us).
+template <class FORM>
+__device__ __forceinline__ float result(const v16f &acc, int r)
+{
+    if constexpr (FORM::TP * FORM::TQ >= 16) {
+        float x;
+        asm("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[r]));
+        return x;
+    } else {
+        return acc[r];
+    }
+}
+// ... behind the last products: the compiler does not know that the moves read what the matrix cores have yet to write (at most 19 cycles later)
+template <class FORM>
+__device__ __forceinline__ void results_ready(v16f (&acc)[FORM::TP][FORM::TQ])
+{
+    if constexpr (FORM::TP == 4 && FORM::TQ == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[i][0]), "+a"(acc[i][1]), "+a"(acc[i][2]), "+a"(acc[i][3]));
+    }
+}
+
 // epilogue(acc, p0, q0, split, staging, lane): first entries of the wave's part of a tile; stores at least EPILOGUE::kStores times for a wave or waits for its stores.
 template <class FORM, class OP, bool PLANES, class EPILOGUE>
 __device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
@@ -379,6 +403,7 @@ __device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
         const int count = min(job.k_per, job.nk - u.split * job.k_per);
         step(Yes{});
         for (int k = 1; k < count; ++k) step(No{});
+        results_ready<FORM>(acc);
         int own = lane;
         asm volatile("" : "+v"(own));      // (what the results' places are made of is formed here, not held through the loop)
         // the wave's own part of the free slot of P, which its own next loads fill; every wave has left that K-tile
@@ -429,7 +454,7 @@ __device__ __forceinline__ void store_strips(const v16f (&acc)[FORM::TP][FORM::T
                 for (int r = 0; r < 4; ++r) {
                     four_t v;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = (T)f(acc[i0 + i][j][4 * r + k], (i0 + i) * 32 + 8 * r + k, j);
+                    for (int k = 0; k < 4; ++k) v[k] = (T)f(result<FORM>(acc[i0 + i][j], 4 * r + k), (i0 + i) * 32 + 8 * r + k, j);
                     const int byte = (i * 32 + 8 * r) * S + 4 * half * S;
                     *reinterpret_cast<four_t *>(staging + row * kRow + (((byte >> 4) ^ swz) << 4) + (byte & 15)) = v;
                 }

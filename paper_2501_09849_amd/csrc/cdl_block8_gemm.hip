@@ -23,9 +23,9 @@ struct Store {
 
 template <class FORM, int FP, int FQ, bool EXACT, class T>
 __global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
-void block8_gemm_kernel(RingJob job, Store<FORM, T> store)
+void block8_gemm_kernel(RingCall<Store<FORM, T>> call)
 {
-    ring<FORM, OpF8<FP, FQ, EXACT>, false>(job, store);
+    ring<FORM, OpF8<FP, FQ, EXACT>, false>(call);
 }
 
 // The parts of a split contraction added up, in order.
@@ -92,7 +92,7 @@ int launch_form(const RingJob &job, int a_format, int b_format, const Store<FORM
     const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, FORM::kLds);
     if (e != hipSuccess) return hip_failed(e);
     const int64_t grid = ring_blocks((int64_t)job.tiles_p * job.tiles_q * job.splits, FORM::PER_CU);
-    CDL_LAUNCH("block8_gemm_kernel", stream, kernel, dim3((unsigned)grid), dim3(FORM::kThreads), FORM::kLds, job, store);
+    CDL_LAUNCH("block8_gemm_kernel", stream, kernel, dim3((unsigned)grid), dim3(FORM::kThreads), FORM::kLds, (RingCall<Store<FORM, T>>{ring_ready(job), store}));
     return check_launch();
 }
 

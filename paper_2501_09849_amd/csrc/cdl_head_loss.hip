@@ -52,11 +52,14 @@ struct Reduce {
 #pragma unroll
         for (int j = 0; j < TQ; ++j) {
             float m = -INFINITY, s = 0.0f;
-            auto value = [&](int i, int r) { return FULL || i * 32 + 8 * (r >> 2) + (r & 3) < left ? result<FORM>(acc[i][j], r) : -INFINITY; };
+            int end = left;
+            asm volatile("" : "+v"(end));      // (compared anew each time: the masks of all entries would take more scalar registers than there are)
+            auto value = [&](int i, int r) { return FULL || i * 32 + 8 * (r >> 2) + (r & 3) < end ? result<FORM>(acc[i][j], r) : -INFINITY; };
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) m = fmaxf(m, value(i, r));
+            asm volatile("" : "+v"(end));
             m = fmaxf(m, __shfl_xor(m, 32, 64));
             const float shift = -m * kLog2e;
 #pragma unroll
@@ -75,9 +78,9 @@ struct Reduce {
 
 template <class FORM, bool PARTS>
 __global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
-void head_reduce_kernel(RingJob job, Reduce<FORM> reduce)
+void head_reduce_kernel(RingCall<Reduce<FORM>> call)
 {
-    ring<FORM, OpBf16, PARTS>(job, reduce);
+    ring<FORM, OpBf16, PARTS>(call);
 }
 
 // A block: 16 tokens, whose stretches 64 threads each add up.
@@ -234,7 +237,7 @@ struct Gradient {
     }
     __device__ __forceinline__ void operator()(const v16f (&acc)[FORM::TP][FORM::TQ], int p0, int q0, int, uint8_t *staging, int lane) const
     {
-        const int half = lane >> 5, left = p0 + FORM::TP * 32 <= cols ? FORM::TP * 32 : cols - p0 - 4 * half;
+        const int half = lane >> 5, left = cols - p0 - 4 * half;
         float factor[FORM::TQ], lse[FORM::TQ];
 #pragma unroll
         for (int j = 0; j < FORM::TQ; ++j) {
@@ -246,29 +249,31 @@ struct Gradient {
                               [&](float z) { return probability(z, lse[j]); });
             __builtin_amdgcn_sched_barrier(0);
         }
-        auto g = [&](float z, int p, int j) {
-            const float x = probability(z, lse[j]) * factor[j];
-            return p < left ? x : 0.0f;
+        auto g = [&](float z, int, int j) { return probability(z, lse[j]) * factor[j]; };
+        auto edge = [&](float z, int p, int j) {
+            int end = left;
+            asm("" : "+v"(end) : "v"(z));      // (compared anew each time: the masks of all entries would take more scalar registers than there are)
+            return p < end ? g(z, p, j) : 0.0f;
         };
-        store_rows<FORM, bf16_t, false>(acc, to, p0, q0, staging, lane, g);
+        store_rows<FORM, bf16_t, false>(acc, to, p0, q0, staging, lane, cols, g, edge);
         if (PARTS) {
             RowTarget<bf16_t> at = to;
             at.out += plane;
-            store_rows<FORM, bf16_t, false>(acc, at, p0, q0, staging, lane, [&](float z, int p, int j) { const float x = g(z, p, j); return x - (float)(bf16_t)x; });
+            auto second = [](float x) { return x - (float)(bf16_t)x; };
+            store_rows<FORM, bf16_t, false>(acc, at, p0, q0, staging, lane, cols, [&](float z, int p, int j) { return second(g(z, p, j)); },
+                                            [&](float z, int p, int j) { return second(edge(z, p, j)); });
             at.out += plane;
-            store_rows<FORM, bf16_t, false>(acc, at, p0, q0, staging, lane, [&](float z, int p, int j) {
-                const float x = g(z, p, j), y = x - (float)(bf16_t)x;
-                return y - (float)(bf16_t)y;
-            });
+            store_rows<FORM, bf16_t, false>(acc, at, p0, q0, staging, lane, cols, [&](float z, int p, int j) { return second(second(g(z, p, j))); },
+                                            [&](float z, int p, int j) { return second(second(edge(z, p, j))); });
         }
     }
 };
 
 template <class FORM, bool PARTS>
 __global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
-void head_gradient_kernel(RingJob job, Gradient<FORM, PARTS> gradient)
+void head_gradient_kernel(RingCall<Gradient<FORM, PARTS>> call)
 {
-    ring<FORM, OpBf16, PARTS>(job, gradient);
+    ring<FORM, OpBf16, PARTS>(call);
 }
 
 // the targets: what is left out above
@@ -308,9 +313,9 @@ struct Store {
 
 template <class FORM, bool PARTS, class T, bool ADD>
 __global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
-void head_product_kernel(RingJob job, Store<FORM, T, ADD> store)
+void head_product_kernel(RingCall<Store<FORM, T, ADD>> call)
 {
-    ring<FORM, OpBf16, PARTS>(job, store);
+    ring<FORM, OpBf16, PARTS>(call);
 }
 
 template <class T>
@@ -433,7 +438,7 @@ int launch_ring(const char *name, KERNEL kernel, int lds, int threads, int per_c
     const hipError_t err = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (err != hipSuccess) return hip_failed(err);
     const int64_t grid = ring_blocks((int64_t)job.tiles_p * job.tiles_q * job.splits, per_cu);
-    CDL_LAUNCH(name, stream, kernel, dim3((unsigned)grid), dim3((unsigned)threads), lds, job, e);
+    CDL_LAUNCH(name, stream, kernel, dim3((unsigned)grid), dim3((unsigned)threads), lds, (RingCall<EPILOGUE>{ring_ready(job), e}));
     return check_launch();
 }
 #define CDL_RING(NAME, FORM, KERNEL, JOB, E, STREAM) launch_ring(NAME, KERNEL, FORM::kLds, FORM::kThreads, FORM::PER_CU, JOB, E, STREAM)

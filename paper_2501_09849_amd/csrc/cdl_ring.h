@@ -60,16 +60,44 @@ struct RingJob {
     int64_t plane_p, plane_q;
     const uint8_t *sp, *sq;        // scales: [K-tile][pitch], pitches multiples of 128
     int64_t pitch_sp, pitch_sq;
+    uint64_t by_tiles, by_group;   // 1 / (tiles_p tiles_q) and 1 / (4 tiles_p), of a launch: ring_ready()
 };
+
+// n / d for n < 2^31 as a product: 2^63 / d rounded up, off by less than 1, makes the quotient too large by less than n / 2^63 < 1 / d.  (The compiler's division by a number
+// that is not known takes some 30 instructions one behind the other; a tile needed twelve of them, 1 us.)
+inline uint64_t reciprocal(uint64_t d) { return ((1ull << 63) + d - 1) / d; }
+__device__ __forceinline__ int divide(int n, uint64_t by) { return (int)__umul64hi((uint64_t)(uint32_t)n << 1, by); }
+
+// What a kernel of this loop is launched with, its only argument.  Between the tiles it is read again from where the launch put it (start(), the epilogue): scalar
+// registers do not hold it all through the loop beside what the loop needs, and what the compiler spilled came back from memory in every K-tile.
+template <class EPILOGUE>
+struct RingCall {
+    RingJob job;
+    EPILOGUE epilogue;
+};
+template <class CALL>
+__device__ __forceinline__ const CALL &again(const CALL &)
+{
+    uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(const CALL *)(const __attribute__((address_space(4))) CALL *)at;
+}
+
+inline RingJob ring_ready(RingJob job)
+{
+    job.by_tiles = reciprocal((uint64_t)job.tiles_p * (uint64_t)job.tiles_q);
+    job.by_group = reciprocal(4 * (uint64_t)job.tiles_p);
+    return job;
+}
 
 // Tile of a unit of work: groups of four rows of tiles, column by column, so that tiles worked on together share rows and columns.
 struct RingUnit { int p0, q0, split; };
 template <class FORM>
 __device__ __forceinline__ RingUnit ring_unit(const RingJob &job, int unit)
 {
-    const int tiles = job.tiles_p * job.tiles_q, split = unit / tiles, t = unit - split * tiles;
-    const int group = t / (4 * job.tiles_p), in = t - group * 4 * job.tiles_p, high = min(4, job.tiles_q - 4 * group);
-    const int p = in / high, q = 4 * group + in - p * high;
+    const int split = divide(unit, job.by_tiles), t = unit - split * job.tiles_p * job.tiles_q;
+    const int group = divide(t, job.by_group), in = t - group * 4 * job.tiles_p, high = min(4, job.tiles_q - 4 * group);
+    const int p = high == 4 ? in >> 2 : high == 3 ? (int)((uint32_t)in / 3u) : in >> (high - 1), q = 4 * group + in - p * high;
     return {p * FORM::kP, q * FORM::kQ, split};
 }
 
@@ -155,7 +183,7 @@ struct OpF8 {
 template <class FORM, bool PLANES, bool IS_P>
 struct RingStream {
     static constexpr int kLoads = IS_P ? FORM::kLoadsP : FORM::kLoadsQ, kBack = 4096;      // (offsets stay positive)
-    int unit, left, end, product;
+    int unit, left, end, product, rows_in;
     const uint8_t *src, *src_s;
     uint32_t off[kLoads], off_s;
     int64_t step_s;
@@ -163,20 +191,34 @@ struct RingStream {
     // parts multiplied, of P and of Q: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
     static __device__ __forceinline__ int part(int product) { return ((IS_P ? 0x850 : 0x244) >> (2 * product)) & 3; }
 
-    __device__ __forceinline__ void start(const RingJob &job, int wave, int lane)
+    struct Place {
+        const uint8_t *src;
+        int left, product;
+    };
+    __device__ __forceinline__ void start(const RingJob &job, int wave, int lane) { go(of_unit(job, wave, lane)); }
+    __device__ __forceinline__ void go(const Place &to)
+    {
+        src = to.src;
+        left = to.left;
+        product = to.product;
+    }
+    __device__ __forceinline__ Place of_unit(const RingJob &job, int wave, int lane)
     {
         const RingUnit u = ring_unit<FORM>(job, unit);
         const int kt = u.split * job.k_per, row0 = IS_P ? u.p0 : u.q0, rows = IS_P ? job.rowsP : job.rowsQ;
         const int64_t ld = IS_P ? job.ldp : job.ldq;
         end = min(kt + job.k_per, job.nk);
-        product = PLANES ? kt / job.plane_nk : 0;
-        const int in_plane = PLANES ? kt - product * job.plane_nk : kt;
-        left = PLANES ? min(job.plane_nk - in_plane, end - kt) : end - kt;
-        src = (IS_P ? job.P : job.Q) + (int64_t)row0 * ld + (int64_t)in_plane * kRingRow + (PLANES ? part(product) * (IS_P ? job.plane_p : job.plane_q) : 0) - kBack;
+        const int product = PLANES ? kt / job.plane_nk : 0, in_plane = PLANES ? kt - product * job.plane_nk : kt;
+        const int left = PLANES ? min(job.plane_nk - in_plane, end - kt) : end - kt;
+        const uint8_t *const src = (IS_P ? job.P : job.Q) + (int64_t)row0 * ld + (int64_t)in_plane * kRingRow + (PLANES ? part(product) * (IS_P ? job.plane_p : job.plane_q) : 0) - kBack;
+        const int most = min(rows - 1 - row0, (IS_P ? FORM::kP : FORM::kQ) - 1);
+        if (most != rows_in) {
+            rows_in = most;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {      // load i fills LDS rows 8 n ... 8 n + 7, chunk c of a row at c ^ (row / 2); rows beyond the matrix: its last one again, whose results nobody stores
-            const int n = wave * kLoads + i;
-            off[i] = (uint32_t)min(n * 8 + (lane >> 3), rows - 1 - row0) * (uint32_t)ld + (uint32_t)((lane & 7) ^ ((4 * n + (lane >> 4)) & 7)) * 16 + kBack - (i & 3) * 1024;
+            for (int i = 0; i < kLoads; ++i) {      // load i fills LDS rows 8 n ... 8 n + 7, chunk c of a row at c ^ (row / 2); rows beyond the matrix: its last one again, whose results nobody stores
+                const int n = wave * kLoads + i;
+                off[i] = (uint32_t)min(n * 8 + (lane >> 3), most) * (uint32_t)ld + (uint32_t)((lane & 7) ^ ((4 * n + (lane >> 4)) & 7)) * 16 + kBack - (i & 3) * 1024;
+            }
         }
         if (FORM::SCALES && !IS_P) {      // four bytes a lane; half of the waves load those of Q, the others those of P
             const bool q = wave & 1;
@@ -186,21 +228,22 @@ struct RingStream {
             off_s = (uint32_t)min((int64_t)lane * 4, pitch - 4 - at);
             step_s = pitch;
         }
+        return {src, left, product};
     }
-    __device__ __forceinline__ void change(const RingJob &job, int each, int last, int wave, int lane)
+    __device__ __forceinline__ Place of_next(const RingJob &job, int each, int last, int wave, int lane)
     {
         if (PLANES) {
             const int next = (product + 1) * job.plane_nk;
             if (next < end) {
-                ++product;
-                src += (part(product) - part(product - 1)) * (IS_P ? job.plane_p : job.plane_q) - (int64_t)job.plane_nk * kRingRow;
-                left = min(job.plane_nk, end - next);
-                return;
+                const int64_t parts = part(product + 1) - part(product);
+                return {src + parts * (IS_P ? job.plane_p : job.plane_q) - (int64_t)job.plane_nk * kRingRow, min(job.plane_nk, end - next), product + 1};
             }
         }
         unit = min(unit + each, last);      // (past the last unit: the last one again, which nobody reads)
-        start(job, wave, lane);
+        return of_unit(job, wave, lane);
     }
+    // (one set of stores for both ways: the compiler would join stores to different members, and keep the members in memory)
+    __device__ __forceinline__ void change(const RingJob &job, int each, int last, int wave, int lane) { go(of_next(job, each, last, wave, lane)); }
     // loads FROM .. TO - 1 of a K-tile
     template <int FROM, int TO>
     __device__ __forceinline__ void issue(uint8_t *slot, int wave) const
@@ -258,8 +301,9 @@ __device__ __forceinline__ void results_ready(v16f (&acc)[FORM::TP][FORM::TQ])
 
 // epilogue(acc, p0, q0, split, staging, lane): first entries of the wave's part of a tile; stores at least EPILOGUE::kStores times for a wave or waits for its stores.
 template <class FORM, class OP, bool PLANES, class EPILOGUE>
-__device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
+__device__ __forceinline__ void ring(const RingCall<EPILOGUE> &call)
 {
+    const RingJob &job = call.job;
     constexpr int TP = FORM::TP, TQ = FORM::TQ, KS = OP::KS;
     extern __shared__ __attribute__((aligned(16))) uint8_t ring_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -273,6 +317,7 @@ __device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
     RingStream<FORM, PLANES, true> from_p;
     RingStream<FORM, PLANES, false> from_q;
     from_p.unit = from_q.unit = first;
+    from_p.rows_in = from_q.rows_in = -1;
     from_p.start(job, wave, lane);
     from_q.start(job, wave, lane);
 
@@ -314,7 +359,7 @@ __device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
         free_p = free_p == (FORM::NP - 1) * FORM::kSlotP ? 0 : free_p + FORM::kSlotP;
         from_p.src += kRingRow;
         __builtin_amdgcn_sched_barrier(0);
-        if (--from_p.left == 0) from_p.change(job, each, total - 1, wave, lane);
+        if (--from_p.left == 0) from_p.change(again(call).job, each, total - 1, wave, lane);
     };
     auto issue_q = [&]() {
         from_q.template issue<0, FORM::kLoadsQ>(ring_lds + FORM::kAtQ + free_q, wave);
@@ -325,7 +370,7 @@ __device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
         if (FORM::SCALES) free_s = free_s == (FORM::NQ - 1) * FORM::kSlotS ? 0 : free_s + FORM::kSlotS;
         from_q.src += kRingRow;
         __builtin_amdgcn_sched_barrier(0);
-        if (--from_q.left == 0) from_q.change(job, each, total - 1, wave, lane);
+        if (--from_q.left == 0) from_q.change(again(call).job, each, total - 1, wave, lane);
     };
     auto barrier = [&]() {
         asm volatile("" ::: "memory");
@@ -399,8 +444,8 @@ __device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
     barrier();
     read(0, Zero{});
     for (int unit = first; unit < end; unit += each) {
-        const RingUnit u = ring_unit<FORM>(job, unit);
-        const int count = min(job.k_per, job.nk - u.split * job.k_per);
+        const RingCall<EPILOGUE> &now = again(call);
+        const int from = ring_unit<FORM>(now.job, unit).split * now.job.k_per, count = min(now.job.k_per, now.job.nk - from);
         step(Yes{});
         for (int k = 1; k < count; ++k) step(No{});
         results_ready<FORM>(acc);
@@ -408,7 +453,9 @@ __device__ __forceinline__ void ring(const RingJob &job, EPILOGUE &epilogue)
         asm volatile("" : "+v"(own));      // (what the results' places are made of is formed here, not held through the loop)
         // the wave's own part of the free slot of P, which its own next loads fill; every wave has left that K-tile
         uint8_t *const staging = ring_lds + (FORM::kTogether || FORM::kLds > FORM::kAtStaging ? FORM::kAtStaging + wave * FORM::STAGING : free_p + wave * FORM::kLoadsP * 1024);
-        epilogue(acc, u.p0 + wp * TP * 32, u.q0 + wq * TQ * 32, u.split, staging, own);
+        const RingCall<EPILOGUE> &then = again(call);
+        const RingUnit u = ring_unit<FORM>(then.job, unit);
+        then.epilogue(acc, u.p0 + wp * TP * 32, u.q0 + wq * TQ * 32, u.split, staging, own);
         stored = true;
         read(0, Zero{});      // (again: the fragments would take registers that the results need)
     }
@@ -444,79 +491,102 @@ __device__ __forceinline__ void store_strips(const v16f (&acc)[FORM::TP][FORM::T
     const int row = lane & 31, half = lane >> 5, swz = row / kTurn & (kChunks - 1);
     const int rr0 = lane / kChunks, c = lane % kChunks;      // of the first read; kStep rows further with each
     T *base = to.out + (int64_t)(q0 + rr0) * to.ld + p0 + c * (16 / S);
+    constexpr int kAcross = TP / kTiles, kStrips = TQ * kAcross;
+    four_t mine[kTiles][4];      // of the strip at hand: taken from the accumulators while the strip before it comes back from LDS
+    auto take = [&](int strip) {
+        const int j = strip / kAcross, i0 = strip % kAcross * kTiles;
 #pragma unroll
-    for (int j = 0; j < TQ; ++j)
+        for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (int i0 = 0; i0 < TP; i0 += kTiles) {
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i)
+                for (int k = 0; k < 4; ++k) mine[i][r][k] = (T)f(result<FORM>(acc[i0 + i][j], 4 * r + k), (i0 + i) * 32 + 8 * r + k, j);
+    };
+    take(0);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    four_t v;
+    for (int strip = 0; strip < kStrips; ++strip) {
+        const int j = strip / kAcross, i0 = strip % kAcross * kTiles;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = (T)f(result<FORM>(acc[i0 + i][j], 4 * r + k), (i0 + i) * 32 + 8 * r + k, j);
-                    const int byte = (i * 32 + 8 * r) * S + 4 * half * S;
-                    *reinterpret_cast<four_t *>(staging + row * kRow + (((byte >> 4) ^ swz) << 4) + (byte & 15)) = v;
-                }
-            asm volatile("" ::: "memory");
-            const int p_at = p0 + i0 * 32, q_at = q0 + j * 32;
-            if (FULL || to.width == 16) {
-                T *at[kReads];
-                u32x4 v[kReads];
-                bool inside[kReads];
+        for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-                for (int n = 0; n < kReads; ++n) {
-                    const int rr = rr0 + n * kStep;
-                    inside[n] = FULL || (p_at + c * (16 / S) < to.rows_p && q_at + rr < to.rows_q);
-                    at[n] = base + (int64_t)(j * 32 + n * kStep) * to.ld + i0 * 32;
-                    v[n] = *reinterpret_cast<const u32x4 *>(staging + rr * kRow + ((c ^ (rr / kTurn & (kChunks - 1))) << 4));
-                }
-                if (ADD) {
-                    f32x4 old[kReads];
+            for (int r = 0; r < 4; ++r) {
+                const int byte = (i * 32 + 8 * r) * S + 4 * half * S;
+                *reinterpret_cast<four_t *>(staging + row * kRow + (((byte >> 4) ^ swz) << 4) + (byte & 15)) = mine[i][r];
+            }
+        asm volatile("" ::: "memory");
+        const int p_at = p0 + i0 * 32, q_at = q0 + j * 32;
+        if (FULL || to.width == 16) {
+            T *at[kReads];
+            u32x4 v[kReads];
+            bool inside[kReads];
 #pragma unroll
-                    for (int n = 0; n < kReads; ++n)
-                        if (inside[n]) old[n] = *reinterpret_cast<const f32x4 *>(at[n]);
-#pragma unroll
-                    for (int n = 0; n < kReads; ++n) {
-                        union { u32x4 u; f32x4 x; } sum{v[n]};
-                        sum.x += old[n];
-                        v[n] = sum.u;
-                    }
-                }
+            for (int n = 0; n < kReads; ++n) {
+                const int rr = rr0 + n * kStep;
+                inside[n] = FULL || (p_at + c * (16 / S) < to.rows_p && q_at + rr < to.rows_q);
+                at[n] = base + (int64_t)(j * 32 + n * kStep) * to.ld + i0 * 32;
+                v[n] = *reinterpret_cast<const u32x4 *>(staging + rr * kRow + ((c ^ (rr / kTurn & (kChunks - 1))) << 4));
+            }
+            f32x4 old[kReads];
+            if (ADD) {
 #pragma unroll
                 for (int n = 0; n < kReads; ++n)
-                    if (inside[n]) *reinterpret_cast<u32x4 *>(at[n]) = v[n];
-            } else {
-                // rows that start anywhere: words, or halves, side by side
-                auto pieces = [&](auto *piece) {
-                    typedef std::remove_pointer_t<decltype(piece)> piece_t;
-                    constexpr int kPer = kRow / (int)sizeof(piece_t);
-                    for (int n = lane; n < 32 * kPer; n += 64) {
-                        const int rr = n / kPer, byte = n % kPer * (int)sizeof(piece_t), p = p_at + byte / S, q = q_at + rr;
-                        if (p >= to.rows_p || q >= to.rows_q) continue;
-                        const piece_t x = *reinterpret_cast<const piece_t *>(staging + rr * kRow + (((byte >> 4) ^ (rr / kTurn & (kChunks - 1))) << 4) + (byte & 15));
-                        piece_t *const at = reinterpret_cast<piece_t *>(to.out + (int64_t)q * to.ld + p);
-                        if constexpr (ADD) *at += x;
-                        else *at = x;
-                    }
-                };
-                if constexpr (S == 4) pieces((float *)nullptr);
-                else if (to.width == 4) pieces((uint32_t *)nullptr);
-                else pieces((uint16_t *)nullptr);
+                    if (inside[n]) old[n] = *reinterpret_cast<const f32x4 *>(at[n]);
             }
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);      // (one strip's registers at a time)
+            if (FULL) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (strip + 1 < kStrips) take(strip + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (ADD) {
+#pragma unroll
+                for (int n = 0; n < kReads; ++n) {
+                    union { u32x4 u; f32x4 x; } sum{v[n]};
+                    sum.x += old[n];
+                    v[n] = sum.u;
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < kReads; ++n)
+                if (inside[n]) *reinterpret_cast<u32x4 *>(at[n]) = v[n];
+        } else {
+            // rows that start anywhere: words, or halves, side by side
+            auto pieces = [&](auto *piece) {
+                typedef std::remove_pointer_t<decltype(piece)> piece_t;
+                constexpr int kPer = kRow / (int)sizeof(piece_t);
+                for (int n = lane; n < 32 * kPer; n += 64) {
+                    const int rr = n / kPer, byte = n % kPer * (int)sizeof(piece_t), p = p_at + byte / S, q = q_at + rr;
+                    if (p >= to.rows_p || q >= to.rows_q) continue;
+                    const piece_t x = *reinterpret_cast<const piece_t *>(staging + rr * kRow + (((byte >> 4) ^ (rr / kTurn & (kChunks - 1))) << 4) + (byte & 15));
+                    piece_t *const at = reinterpret_cast<piece_t *>(to.out + (int64_t)q * to.ld + p);
+                    if constexpr (ADD) *at += x;
+                    else *at = x;
+                }
+            };
+            if constexpr (S == 4) pieces((float *)nullptr);
+            else if (to.width == 4) pieces((uint32_t *)nullptr);
+            else pieces((uint16_t *)nullptr);
         }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);      // (one strip's registers at a time)
+        if (!FULL && strip + 1 < kStrips) take(strip + 1);
+    }
+}
+// edge: f where the wave's part may reach beyond the entry `end`
+template <class FORM, class T, bool ADD, class F, class G>
+__device__ __forceinline__ void store_rows(const v16f (&acc)[FORM::TP][FORM::TQ], const RowTarget<T> &to, int p0, int q0, uint8_t *staging, int lane, int end, const F &f,
+                                           const G &edge)
+{
+    if (p0 + FORM::TP * 32 <= end && q0 + FORM::TQ * 32 <= to.rows_q && to.width == 16) {
+        store_strips<FORM, T, ADD, true>(acc, to, p0, q0, staging, lane, f);
+    } else {
+        store_strips<FORM, T, ADD, false>(acc, to, p0, q0, staging, lane, edge);
+        __builtin_amdgcn_s_waitcnt(wait_imm(0));
+    }
 }
 template <class FORM, class T, bool ADD, class F>
 __device__ __forceinline__ void store_rows(const v16f (&acc)[FORM::TP][FORM::TQ], const RowTarget<T> &to, int p0, int q0, uint8_t *staging, int lane, const F &f)
 {
-    if (p0 + FORM::TP * 32 <= to.rows_p && q0 + FORM::TQ * 32 <= to.rows_q && to.width == 16) {
-        store_strips<FORM, T, ADD, true>(acc, to, p0, q0, staging, lane, f);
-    } else {
-        store_strips<FORM, T, ADD, false>(acc, to, p0, q0, staging, lane, f);
-        __builtin_amdgcn_s_waitcnt(wait_imm(0));
-    }
+    store_rows<FORM, T, ADD>(acc, to, p0, q0, staging, lane, to.rows_p, f, f);
 }
 // stores of a wave where its part is whole
 template <class FORM, class T>

@@ -65,19 +65,23 @@ struct Layout {
     int tiles_p, tiles_q, splits, k_per;
 };
 
+// Wide where it keeps the chip busy, half of the compute units at least over 24 K-tiles; Thin, two blocks of which a compute unit holds, for few tokens and for products that
+// are less than one tile of 128 x 128 for each compute unit (us, results bf16: 1000 x 1000 x 520 9.4 as Square, 8.0 as Thin; x 4096 21.6, 16.5; 1700 x 1700 x 2048 20.4, 17.7).
+// The contraction is split where tiles are few and it is 48 K-tiles long, into parts of 16 at least: adding the parts up takes a launch, 8 us (1000 x 1000 x 2048
+// in two parts 22.1, in one 11.7; 4 x 8192 x 8192 in eight parts 24.0, in four 21.5).
 Layout layout(int32_t M, int32_t N, int32_t K)
 {
     const int nk = (int)(block8_pitch(K) / kRingRow);
     Layout l;
-    const int64_t wide = (int64_t)((M + 255) / 256) * ((N + 255) / 256);
-    l.form = M <= 64 ? kThin : wide * nk >= 24 * 128 ? kWide : kSquare;
+    const int64_t wide = (int64_t)((M + 255) / 256) * ((N + 255) / 256), square = (int64_t)((M + 127) / 128) * ((N + 127) / 128);
+    l.form = M <= 64 ? kThin : wide * nk >= 24 * 128 ? kWide : square < 256 ? kThin : kSquare;
     const int p = l.form == kWide ? 256 : 128, q = l.form == kWide ? 256 : l.form == kSquare ? 128 : 64, per_cu = l.form == kThin ? 2 : 1;
     l.tiles_p = (N + p - 1) / p;
     l.tiles_q = (M + q - 1) / q;
     const int64_t tiles = (int64_t)l.tiles_p * l.tiles_q, places = 256 * per_cu;
+    const int64_t most = nk < 48 ? 1 : nk / 16;
     int64_t splits = tiles >= places ? 1 : places / tiles;
-    splits = splits < nk / 4 ? splits : nk / 4;
-    if (splits < 1) splits = 1;
+    splits = splits < most ? splits : most;
     const int per = (int)((nk + splits - 1) / splits);
     l.splits = (nk + per - 1) / per;
     l.k_per = per;

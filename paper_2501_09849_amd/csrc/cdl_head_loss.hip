@@ -83,32 +83,45 @@ void head_reduce_kernel(RingCall<Reduce<FORM>> call)
     ring<FORM, OpBf16, PARTS>(call);
 }
 
-// A block: 16 tokens, whose stretches 64 threads each add up.
-constexpr int kFinishTokens = 16, kFinishThreads = 1024;
+// A block: 1 << bits tokens side by side, whose stretches the other threads share, eight at a time so that as many loads are under way.
+// 16 tokens a block where that makes enough blocks, 4 for fewer tokens (16 tokens, 1564 stretches: 4 a block 8.1 us, 16 a block 10.7; 8192 tokens, 391 stretches: 29 and 11).
+constexpr int kFinishThreads = 1024;
+constexpr int finish_bits(int64_t tokens) { return tokens > 1024 ? 4 : 2; }
+__device__ __forceinline__ float scaled(float x, float from, float top) { return x * (from == top ? 1.0f : expf(from - top)); }      // (equal ones, also infinite: no difference of infinities)
 __global__ __launch_bounds__(kFinishThreads)
 void head_finish_kernel(const float2 *__restrict__ partial, int stretches, const float *__restrict__ at_target, const int64_t *__restrict__ target, int tokens, int V,
-                        float *__restrict__ loss, float *__restrict__ lse)
+                        int bits, float *__restrict__ loss, float *__restrict__ lse)
 {
-    __shared__ float2 part[64][kFinishTokens];
-    const int tid = threadIdx.x, own = tid & 15, group = tid >> 4, t = blockIdx.x * kFinishTokens + own;
+    __shared__ float2 part[16][16];
+    const int tid = threadIdx.x, own = tid & ((1 << bits) - 1), group = tid >> bits, groups = kFinishThreads >> bits, t = (int)(blockIdx.x << bits) + own;
     float m = -INFINITY, s = 0.0f;
     if (t < tokens)
-        for (int i = group; i < stretches; i += 64) {
-            const float2 x = partial[(int64_t)i * tokens + t];
-            const float top = fmaxf(m, x.x);
-            // (equal largest ones, also infinite: no difference of infinities)
-            s = s * (m == top ? 1.0f : expf(m - top)) + x.y * (x.x == top ? 1.0f : expf(x.x - top));
+        for (int i = group; i < stretches; i += 8 * groups) {
+            float2 x[8];
+            float top = m;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = i + k * groups < stretches ? partial[(int64_t)(i + k * groups) * tokens + t] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = fmaxf(top, x[k].x);
+            s = scaled(s, m, top);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += scaled(x[k].y, x[k].x, top);
             m = top;
         }
-    part[group][own] = make_float2(m, s);
+    // the lanes of a wave, then the waves
+    for (int step = 1 << bits; step < 64; step <<= 1) {
+        const float m2 = __shfl_xor(m, step, 64), s2 = __shfl_xor(s, step, 64), top = fmaxf(m, m2);
+        s = scaled(s, m, top) + scaled(s2, m2, top);
+        m = top;
+    }
+    if ((tid & 63) < 1 << bits) part[tid >> 6][own] = make_float2(m, s);
     __syncthreads();
     if (group != 0 || t >= tokens) return;
     float top = -INFINITY, sum = 0.0f;
-    for (int g = 0; g < 64; ++g) top = fmaxf(top, part[g][own].x);
-    for (int g = 0; g < 64; ++g) {
-        const float2 x = part[g][own];
-        sum += x.y * (x.x == top ? 1.0f : expf(x.x - top));
-    }
+#pragma unroll
+    for (int g = 0; g < 16; ++g) top = fmaxf(top, part[g][own].x);
+#pragma unroll
+    for (int g = 0; g < 16; ++g) sum += scaled(part[g][own].y, part[g][own].x, top);
     const float all = top + logf(sum);
     lse[t] = all;
     if (loss) {
@@ -154,24 +167,23 @@ void head_rows_kernel(const T *__restrict__ x, int64_t rows, int D, int Dp, bf16
 __global__ __launch_bounds__(256)
 void head_transpose_kernel(const bf16_t *__restrict__ x, int64_t ld, int64_t plane, int rows, int cols, bf16_t *__restrict__ out, int64_t ld_out, int64_t plane_out)
 {
-    __shared__ uint16_t tile[64][72];
+    __shared__ __attribute__((aligned(16))) uint32_t tile[64 * 32];      // [column][pair of rows], 16-byte chunks at chunk ^ (column / 8): neither side meets in a bank
     x += blockIdx.z * plane;
     out += blockIdx.z * plane_out;
-    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tid = threadIdx.x;
+    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tid = threadIdx.x, across = tid & 7, pair = tid >> 3;
+    union { u32x4 u; uint16_t h[8]; } v[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int r = i * 32 + (tid >> 3), c = (tid & 7) * 8;
-        union { u32x4 u; uint16_t h[8]; } v;
-        v.u = (u32x4){0, 0, 0, 0};
-        if (r0 + r < rows) v.u = *reinterpret_cast<const u32x4 *>(x + (int64_t)(r0 + r) * ld + c0 + c);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) tile[c + k][r] = v.h[k];
+        v[i].u = (u32x4){0, 0, 0, 0};
+        if (r0 + 2 * pair + i < rows) v[i].u = *reinterpret_cast<const u32x4 *>(x + (int64_t)(r0 + 2 * pair + i) * ld + c0 + 8 * across);
     }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) tile[(8 * across + k) * 32 + (((pair >> 2) ^ across) << 2) + (pair & 3)] = (uint32_t)v[0].h[k] | (uint32_t)v[1].h[k] << 16;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int c = i * 32 + (tid >> 3), r = (tid & 7) * 8;
-        if (c0 + c < cols) *reinterpret_cast<u32x4 *>(out + (int64_t)(c0 + c) * ld_out + r0 + r) = *reinterpret_cast<const u32x4 *>(&tile[c][r]);
+        const int c = i * 32 + pair;
+        if (c0 + c < cols) *reinterpret_cast<u32x4 *>(out + (int64_t)(c0 + c) * ld_out + r0 + 8 * across) = *reinterpret_cast<const u32x4 *>(&tile[c * 32 + ((across ^ (c >> 3)) << 2)]);
     }
 }
 
@@ -185,10 +197,18 @@ void head_unit_kernel(const int64_t *__restrict__ target, const float *__restric
 {
     __shared__ float part[16];
     float m = 0.0f;
-    for (int t = threadIdx.x; t < T; t += 1024) {
-        const int64_t at = target[t];
-        const float a = at >= 0 && at < V ? (d_loss ? fabsf(d_loss[t]) : 1.0f) : 0.0f, b = d_lse ? fabsf(d_lse[t]) : 0.0f;
-        m = fmaxf(m, a + b);
+    for (int t0 = threadIdx.x; t0 < T; t0 += 8 * 1024) {      // eight tokens a thread, all loads under way together
+        int64_t at[8];
+        float a[8], b[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int t = min(t0 + k * 1024, T - 1);
+            at[k] = target[t];
+            a[k] = d_loss ? d_loss[t] : 1.0f;
+            b[k] = d_lse ? d_lse[t] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = fmaxf(m, (at[k] >= 0 && at[k] < V ? fabsf(a[k]) : 0.0f) + fabsf(b[k]));
     }
 #pragma unroll
     for (int s = 32; s; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
@@ -524,8 +544,8 @@ int forward(const T *h, const T *w, int32_t type, const int64_t *target, int32_t
     const RingJob job = ring_job(p.reduce, pw, p.Dp, V, ph, p.Dp, tokens, p.Dp, p.parts, V * p.Dp, tokens * p.Dp);
     float *const at_target = (float *)(ws + p.at_target);
     CDL_TRY(run_reduce<sizeof(T) == 4>(p, job, partial, target, at_target, V, tokens, stream));
-    CDL_LAUNCH("head_finish_kernel", stream, head_finish_kernel, dim3(blocks_of(tokens, kFinishTokens)), dim3(kFinishThreads), 0, (const float2 *)partial,
-               (int)p.stretches, (const float *)at_target, target, tokens, V, loss, lse);
+    CDL_LAUNCH("head_finish_kernel", stream, head_finish_kernel, dim3(blocks_of(tokens, 1 << finish_bits(tokens))), dim3(kFinishThreads), 0, (const float2 *)partial,
+               (int)p.stretches, (const float *)at_target, target, tokens, V, finish_bits(tokens), loss, lse);
     return check_launch();
 }
 

@@ -418,8 +418,10 @@ int cdl_block8_quantize(const void *x, int32_t type, int32_t rows, int32_t cols,
  *   y[m,n] = sum_kb a_scale[kb,m] * b_scale[kb,n] * sum_{k in block kb} a[m,k] * b[n,k]     (y[M,N], fp32 or bf16 by y_type)
  * a [M][pitch(K)] with a_scale [blocks of K][pitch(M)], b [N][pitch(K)] with b_scale [blocks of K][pitch(N)], as
  * cdl_block8_quantize writes them (bytes beyond K have to be zero; scale bytes 1 .. 254).  Into fp32: products are exact and sums
- * fp32 (an entry below 2^-126 in value counts as 0; the quantizer makes none).  Into bf16: the matrix instructions for 8-bit operands, at twice the rate, which of every product keep what lies above 2^-14 of the largest of the 16
- * that they add up first (1.5e-5 of the result over random operands), sums in fp32, one rounding.  With x -> (q, scale) of the activations, w -> tiles of the weights and g -> the gradient of the output,
+ * fp32 (an entry below 2^-126 in value counts as 0; the quantizer makes none).  Into bf16: the matrix instructions for
+ * 8-bit operands, at twice the rate, which of every product keep what lies above 2^-14 of the largest of the 16 that they
+ * add up first (1.5e-5 of the result over random operands), sums in fp32, one rounding.  With x -> (q, scale) of the
+ * activations, w -> tiles of the weights and g -> the gradient of the output,
  *   forward y = x . w^T          a = x,     b = w
  *   d_x = g . w                  a = g,     b = w's (q_t, scale_t)
  *   d_w = g^T . x                a = g's (q_t, scale_t),  b = x's (q_t, scale_t)

@@ -63,19 +63,18 @@ enum Form { kWide, kSquare, kThin };
 struct Layout {
     Form form;
     int tiles_p, tiles_q, splits, k_per;
+    float cost;
 };
 
-// Wide where it keeps the chip busy, half of the compute units at least over 24 K-tiles; Thin, two blocks of which a compute unit holds, for few tokens and for products that
-// are less than one tile of 128 x 128 for each compute unit (us, results bf16: 1000 x 1000 x 520 9.4 as Square, 8.0 as Thin; x 4096 21.6, 16.5; 1700 x 1700 x 2048 20.4, 17.7).
-// The contraction is split where tiles are few and it is 48 K-tiles long, into parts of 16 at least: adding the parts up takes a launch, 8 us (1000 x 1000 x 2048
-// in two parts 22.1, in one 11.7; 4 x 8192 x 8192 in eight parts 24.0, in four 21.5).
-Layout layout(int32_t M, int32_t N, int32_t K)
+// A product in one form, and what it takes, in K-tiles of a block of 128 x 128 alone on its compute unit (0.6 us): rounds of blocks over the chip, 3.3 for a K-tile of
+// 256 x 256, 1.1 for two blocks of 128 x 64 on a compute unit, 0.55 where there is one.  The contraction is split where tiles leave compute units idle and it is
+// 48 K-tiles long, into parts of 16 at least: adding the parts up takes a launch, 8 us, and their way to memory and back (1000 x 1000 x 2048 in two parts 22.1 us, in one
+// 11.7; 4 x 8192 x 8192 in eight parts 24.0, in four 21.5).
+Layout layout_of(Form form, int32_t M, int32_t N, int nk)
 {
-    const int nk = (int)(block8_pitch(K) / kRingRow);
     Layout l;
-    const int64_t wide = (int64_t)((M + 255) / 256) * ((N + 255) / 256), square = (int64_t)((M + 127) / 128) * ((N + 127) / 128);
-    l.form = M <= 64 ? kThin : wide * nk >= 24 * 128 ? kWide : square < 256 ? kThin : kSquare;
-    const int p = l.form == kWide ? 256 : 128, q = l.form == kWide ? 256 : l.form == kSquare ? 128 : 64, per_cu = l.form == kThin ? 2 : 1;
+    l.form = form;
+    const int p = form == kWide ? 256 : 128, q = form == kWide ? 256 : form == kSquare ? 128 : 64, per_cu = form == kThin ? 2 : 1;
     l.tiles_p = (N + p - 1) / p;
     l.tiles_q = (M + q - 1) / q;
     const int64_t tiles = (int64_t)l.tiles_p * l.tiles_q, places = 256 * per_cu;
@@ -85,7 +84,26 @@ Layout layout(int32_t M, int32_t N, int32_t K)
     const int per = (int)((nk + splits - 1) / splits);
     l.splits = (nk + per - 1) / per;
     l.k_per = per;
+    const int64_t units = tiles * l.splits;
+    const float each = form == kWide ? 3.3f : form == kSquare ? 1.0f : units <= 256 ? 0.55f : 1.1f;
+    l.cost = (float)((units + places - 1) / places) * (float)per * each + (l.splits > 1 ? 13.0f + (float)l.splits * (float)M * (float)N * 1.7e-6f : 0.0f);
     return l;
+}
+
+// The form that takes least; for few tokens, of which a wider tile would hold one row of tiles, the thin one.  Results bf16, us, as Wide, Square, Thin:
+//   1000 x 1000 x 520     -    9.4   8.0        2048 x 2048 x 2048   30.4  16.7   -          4096 x 4096 x 768    22.3  25.0   -
+//   1000 x 1000 x 4096    -   21.6  16.5        2048 x 2048 x 8192   56.6  40.1   -          8192 x 4096 x 2048   64.8  78.3   -
+//   1700 x 1700 x 2048    -   20.4  17.7        1024 x 1024 x 16384  43.6  33.4   -          65536 x 1024 x 512   47.1  60.6   -
+Layout layout(int32_t M, int32_t N, int32_t K)
+{
+    const int nk = (int)(block8_pitch(K) / kRingRow);
+    Layout best = layout_of(kThin, M, N, nk);
+    if (M <= 64) return best;
+    for (Form form : {kSquare, kWide}) {
+        const Layout l = layout_of(form, M, N, nk);
+        if (l.cost < best.cost) best = l;
+    }
+    return best;
 }
 
 template <class FORM, bool EXACT, class T>

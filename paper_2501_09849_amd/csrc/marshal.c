@@ -85,6 +85,15 @@ static int get_int_by(PyObject *o, int64_t *v, PyObject *(*convert)(PyObject *))
 }
 static int get_index(PyObject *o, int64_t *v) { return get_int_by(o, v, PyNumber_Index); }
 static int get_int(PyObject *o, int64_t *v) { return get_int_by(o, v, PyNumber_Long); }
+/* an index in [0, 2^64), else an error */
+static int get_unsigned(PyObject *o, uint64_t *v)
+{
+    PyObject *n = PyNumber_Index(o);
+    if (!n) return -1;
+    *v = PyLong_AsUnsignedLongLong(n);
+    Py_DECREF(n);
+    return PyErr_Occurred() ? -1 : 0;
+}
 
 /* a real number of a quantizer, or a scale: as float() converts it */
 static int get_real(PyObject *o, float *v)
@@ -124,10 +133,7 @@ static int parse(const char *name, const char *format, PyObject *const *o, Py_ss
         switch (*c) {
             case 'p': if (get_ptr(o[at++], &a->p[np++])) return -1; break;
             case 'n': if (get_index(o[at++], &a->n)) return -1; break;
-            case 'u':
-                a->u[nu++] = PyLong_AsUnsignedLongLong(o[at++]);      /* (an integer in [0, 2^64), else an error) */
-                if (PyErr_Occurred()) return -1;
-                break;
+            case 'u': if (get_unsigned(o[at++], &a->u[nu++])) return -1; break;
             case 'i': if (get_index(o[at++], &v)) return -1; a->i[ni++] = (int32_t)v; break;
             case 'o': if (get_int(o[at++], &v)) return -1; a->i[ni++] = (int32_t)v; break;
             case 'r': if (get_real(o[at++], &a->f[nf++])) return -1; break;

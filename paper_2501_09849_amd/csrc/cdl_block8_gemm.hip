@@ -25,7 +25,7 @@ template <class FORM, int FP, int FQ, bool EXACT, class T>
 __global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
 void block8_gemm_kernel(RingCall<Store<FORM, T>> call)
 {
-    ring<FORM, OpF8<FP, FQ, EXACT>, false>(call);
+    ring<FORM, OpF8<FP, FQ, EXACT>, false, false, false>(call);
 }
 
 // The parts of a split contraction added up, in order.

@@ -80,7 +80,7 @@ template <class FORM, bool PARTS>
 __global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
 void head_reduce_kernel(RingCall<Reduce<FORM>> call)
 {
-    ring<FORM, OpBf16, PARTS>(call);
+    ring<FORM, OpBf16, PARTS, false, false>(call);
 }
 
 // A block: 1 << bits tokens side by side, whose stretches the other threads share, eight at a time so that as many loads are under way.
@@ -160,30 +160,6 @@ void head_rows_kernel(const T *__restrict__ x, int64_t rows, int D, int Dp, bf16
             to += rows * Dp;
             store8(to, v, false);
         }
-    }
-}
-
-// Rows [rows][ld] -> [cols][ld_out], zeros beyond rows; parts `plane` and `plane_out` entries apart, by blockIdx.z.  ld, ld_out multiples of 64.
-__global__ __launch_bounds__(256)
-void head_transpose_kernel(const bf16_t *__restrict__ x, int64_t ld, int64_t plane, int rows, int cols, bf16_t *__restrict__ out, int64_t ld_out, int64_t plane_out)
-{
-    __shared__ __attribute__((aligned(16))) uint32_t tile[64 * 32];      // [column][pair of rows], 16-byte chunks at chunk ^ (column / 8): neither side meets in a bank
-    x += blockIdx.z * plane;
-    out += blockIdx.z * plane_out;
-    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, tid = threadIdx.x, across = tid & 7, pair = tid >> 3;
-    union { u32x4 u; uint16_t h[8]; } v[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        v[i].u = (u32x4){0, 0, 0, 0};
-        if (r0 + 2 * pair + i < rows) v[i].u = *reinterpret_cast<const u32x4 *>(x + (int64_t)(r0 + 2 * pair + i) * ld + c0 + 8 * across);
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) tile[(8 * across + k) * 32 + (((pair >> 2) ^ across) << 2) + (pair & 3)] = (uint32_t)v[0].h[k] | (uint32_t)v[1].h[k] << 16;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int c = i * 32 + pair;
-        if (c0 + c < cols) *reinterpret_cast<u32x4 *>(out + (int64_t)(c0 + c) * ld_out + r0 + 8 * across) = *reinterpret_cast<const u32x4 *>(&tile[c * 32 + ((across ^ (c >> 3)) << 2)]);
     }
 }
 
@@ -293,7 +269,7 @@ template <class FORM, bool PARTS>
 __global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
 void head_gradient_kernel(RingCall<Gradient<FORM, PARTS>> call)
 {
-    ring<FORM, OpBf16, PARTS>(call);
+    ring<FORM, OpBf16, PARTS, false, false>(call);
 }
 
 // the targets: what is left out above
@@ -331,11 +307,12 @@ struct Store {
     }
 };
 
-template <class FORM, bool PARTS, class T, bool ADD>
+// P the vocabulary or the states, down whose rows the contraction runs, and for the gradient of the vocabulary (DOWN) g too
+template <class FORM, bool PARTS, class T, bool ADD, bool DOWN>
 __global__ __launch_bounds__(FORM::kThreads, FORM::PER_CU)
 void head_product_kernel(RingCall<Store<FORM, T, ADD>> call)
 {
-    ring<FORM, OpBf16, PARTS>(call);
+    ring<FORM, OpBf16, PARTS, true, DOWN>(call);
 }
 
 template <class T>
@@ -393,7 +370,7 @@ constexpr int64_t kPieceEntries = 1 << 27;
 
 struct Plan {
     int parts;
-    int64_t Dp, Tp, Tl;               // up to multiples of 64; pitch of rows of tokens
+    int64_t Dp, Tp;                   // up to multiples of 64
     bool copy;                        // the operands as rows of Dp entries in the workspace
     Form reduce;
     int64_t stretches;
@@ -403,7 +380,7 @@ struct Plan {
     Split split_h;
     int64_t tokens;                   // of the table, whole tiles
     // offsets in the workspace
-    size_t rows_h, rows_w, at_target, partial, unit, table, ht, wt, g, gt, sums, bytes;
+    size_t rows_h, rows_w, at_target, partial, unit, table, g, sums, bytes;
 };
 
 Plan make_plan(int64_t T, int64_t V, int64_t D, int32_t type, bool train)
@@ -412,7 +389,6 @@ Plan make_plan(int64_t T, int64_t V, int64_t D, int32_t type, bool train)
     p.parts = type == CDL_F32 ? 3 : 1;
     p.Dp = D == 0 ? 64 : up(D, 64);
     p.Tp = up(T, 64);
-    p.Tl = line_pitch(p.Tp);
     p.copy = type == CDL_F32 || p.Dp != D;
     p.reduce = choose_form(V, T);
     p.stretches = (V + form_stretch(p.reduce) - 1) / form_stretch(p.reduce);
@@ -441,10 +417,7 @@ Plan make_plan(int64_t T, int64_t V, int64_t D, int32_t type, bool train)
         p.form_w = choose_form(D, p.piece);
         const int64_t tiles = ((D + form_p(p.form_h) - 1) / form_p(p.form_h)) * ((T + form_q(p.form_h) - 1) / form_q(p.form_h));
         p.split_h = choose_splits(tiles < 1 ? 1 : tiles, form_per_cu(p.form_h), (int)(up(p.piece, 64) / 64 * (p.parts == 3 ? 6 : 1)));
-        p.ht = take(p.parts * up(D, 64) * p.Tl * 2);
-        p.wt = take(p.parts * up(D, 64) * p.piece_l * 2);
-        p.g = take(p.parts * T * p.piece_l * 2);
-        p.gt = take(p.parts * p.piece_l * p.Tl * 2);
+        p.g = take(p.parts * p.Tp * p.piece_l * 2);
         p.sums = take((int64_t)p.split_h.splits * T * D * 4);
         if (at < forward) at = forward;
     }
@@ -505,13 +478,13 @@ int run_gradient(const Plan &p, const RingJob &job, const RowTarget<bf16_t> &to,
     }
 }
 
-template <bool PARTS, class T, bool ADD>
+template <bool PARTS, class T, bool ADD, bool DOWN>
 int run_product(Form form, const RingJob &job, const RowTarget<T> &to, int64_t part, const float *by, hipStream_t stream)
 {
     switch (form) {
-        case kWide: return CDL_RING("head_product_kernel", Wide, (head_product_kernel<Wide, PARTS, T, ADD>), job, (Store<Wide, T, ADD>{to, part, by}), stream);
-        case kSquare: return CDL_RING("head_product_kernel", Square, (head_product_kernel<Square, PARTS, T, ADD>), job, (Store<Square, T, ADD>{to, part, by}), stream);
-        default: return CDL_RING("head_product_kernel", Thin, (head_product_kernel<Thin, PARTS, T, ADD>), job, (Store<Thin, T, ADD>{to, part, by}), stream);
+        case kWide: return CDL_RING("head_product_kernel", Wide, (head_product_kernel<Wide, PARTS, T, ADD, DOWN>), job, (Store<Wide, T, ADD>{to, part, by}), stream);
+        case kSquare: return CDL_RING("head_product_kernel", Square, (head_product_kernel<Square, PARTS, T, ADD, DOWN>), job, (Store<Square, T, ADD>{to, part, by}), stream);
+        default: return CDL_RING("head_product_kernel", Thin, (head_product_kernel<Thin, PARTS, T, ADD, DOWN>), job, (Store<Thin, T, ADD>{to, part, by}), stream);
     }
 }
 
@@ -521,13 +494,6 @@ template <class T>
 int to_rows(const T *x, int64_t rows, int64_t D, int64_t Dp, bf16_t *out, hipStream_t stream)
 {
     CDL_LAUNCH("head_rows_kernel", stream, head_rows_kernel<T>, dim3(blocks_of(rows * (Dp / 8), 256)), dim3(256), 0, x, rows, (int)D, (int)Dp, out);
-    return check_launch();
-}
-
-int transpose(const bf16_t *x, int64_t ld, int64_t plane, int64_t rows, int64_t cols, bf16_t *out, int64_t ld_out, int64_t plane_out, int parts, hipStream_t stream)
-{
-    CDL_LAUNCH("head_transpose_kernel", stream, head_transpose_kernel, dim3(blocks_of(cols, 64), blocks_of(rows, 64), (unsigned)parts), dim3(256), 0, x, ld, plane, (int)rows,
-               (int)cols, out, ld_out, plane_out);
     return check_launch();
 }
 
@@ -570,33 +536,33 @@ int backward(const T *h, const T *w, int32_t type, const int64_t *target, const 
     CDL_LAUNCH("head_tokens_kernel", stream, head_tokens_kernel, dim3(blocks_of(p.tokens, 256)), dim3(256), 0, target, lse, d_loss, d_lse, tokens, (int)p.tokens, V,
                (const float *)unit, table);
     CDL_TRY(check_launch());
-    bf16_t *const ht = (bf16_t *)(ws + p.ht), *const wt = (bf16_t *)(ws + p.wt), *const g = (bf16_t *)(ws + p.g), *const gt = (bf16_t *)(ws + p.gt);
-    if (d_w) CDL_TRY(transpose(ph, p.Dp, tokens * p.Dp, tokens, D, ht, p.Tl, up(D, 64) * p.Tl, p.parts, stream));
-    const int64_t plane_g = tokens * p.piece_l;
+    bf16_t *const g = (bf16_t *)(ws + p.g);
+    const int64_t plane_g = p.Tp * p.piece_l;
     for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
         const int64_t cols = v0 + p.piece <= V ? p.piece : V - v0, padded = up(cols, 64);
         const bf16_t *const piece = pw + v0 * p.Dp;
         {
             const RingJob job = ring_job(p.gradient, piece, p.Dp, cols, ph, p.Dp, tokens, p.Dp, p.parts, V * p.Dp, tokens * p.Dp);
-            CDL_TRY(run_gradient<PARTS>(p, job, RowTarget<bf16_t>{g, p.piece_l, (int)padded, tokens, 16}, table, at_target, tokens, (int)v0, (int)cols, plane_g, stream));
+            CDL_TRY(run_gradient<PARTS>(p, job, RowTarget<bf16_t>{g, p.piece_l, (int)padded, (int)p.Tp, 16}, table, at_target, tokens, (int)v0, (int)cols, plane_g, stream));
             CDL_LAUNCH("head_target_kernel", stream, head_target_kernel, dim3(blocks_of(tokens, 256)), dim3(256), 0, (const Token *)table, (const float *)at_target, tokens, (int)v0, (int)cols, g, p.piece_l,
                        plane_g, p.parts);
             CDL_TRY(check_launch());
         }
         if (d_h) {
-            CDL_TRY(transpose(piece, p.Dp, V * p.Dp, cols, D, wt, p.piece_l, up(D, 64) * p.piece_l, p.parts, stream));
-            RingJob job = ring_job(p.form_h, wt, p.piece_l, D, g, p.piece_l, tokens, padded, p.parts, up(D, 64) * p.piece_l, plane_g);
+            RingJob job = ring_job(p.form_h, piece, p.Dp, D, g, p.piece_l, tokens, padded, p.parts, V * p.Dp, plane_g);
+            job.downP = (int)cols;
             job.k_per = p.split_h.k_per;
             job.splits = (job.nk + job.k_per - 1) / job.k_per;      // (a last, shorter piece: fewer parts)
             const RowTarget<float> to{sums, D, D, tokens, row_width(sums, (int64_t)D * 4)};
             const int64_t part = (int64_t)tokens * D;
-            CDL_TRY(v0 == 0 ? (run_product<PARTS, float, false>(p.form_h, job, to, part, nullptr, stream)) : (run_product<PARTS, float, true>(p.form_h, job, to, part, nullptr, stream)));
+            CDL_TRY(v0 == 0 ? (run_product<PARTS, float, false, false>(p.form_h, job, to, part, nullptr, stream)) : (run_product<PARTS, float, true, false>(p.form_h, job, to, part, nullptr, stream)));
         }
         if (d_w) {
-            CDL_TRY(transpose(g, p.piece_l, plane_g, tokens, cols, gt, p.Tl, p.piece_l * p.Tl, p.parts, stream));
-            const RingJob job = ring_job(p.form_w, ht, p.Tl, D, gt, p.Tl, cols, p.Tp, p.parts, up(D, 64) * p.Tl, p.piece_l * p.Tl);
+            RingJob job = ring_job(p.form_w, ph, p.Dp, D, g, p.piece_l, cols, p.Tp, p.parts, tokens * p.Dp, plane_g);
+            job.downP = tokens;
+            job.downQ = (int)p.Tp;
             T *const out = d_w + v0 * D;
-            CDL_TRY((run_product<PARTS, T, false>(p.form_w, job, RowTarget<T>{out, D, D, (int)cols, row_width(out, (int64_t)D * (int64_t)sizeof(T))}, 0, unit, stream)));
+            CDL_TRY((run_product<PARTS, T, false, true>(p.form_w, job, RowTarget<T>{out, D, D, (int)cols, row_width(out, (int64_t)D * (int64_t)sizeof(T))}, 0, unit, stream)));
         }
     }
     if (d_h) {

@@ -60,6 +60,7 @@ struct RingJob {
     int64_t plane_p, plane_q;
     const uint8_t *sp, *sq;        // scales: [K-tile][pitch], pitches multiples of 128
     int64_t pitch_sp, pitch_sq;
+    int downP, downQ;              // rows in memory of an operand whose contraction runs down its rows
     uint64_t by_tiles, by_group;   // 1 / (tiles_p tiles_q) and 1 / (4 tiles_p), of a launch: ring_ready()
 };
 
@@ -180,13 +181,20 @@ struct OpF8 {
 // Where the loads of an operand come from: K-tile after K-tile, `left` of them before change() has to be called, which goes on to the next unit of work (or to
 // the next product of parts).  Four loads share a base in LDS: the instruction's offset counts on both sides, so a lane's offset into memory
 // takes it back.
-template <class FORM, bool PLANES, bool IS_P>
+//
+// DOWN: the contraction runs down the rows of the operand (bf16), which is [k][p]: a K-tile is 64 rows of it, of each the tile's entries side by side, in LDS too.
+// What lies beyond the matrix in memory is read as its last 16 bytes; rows beyond the contraction meet zeros of the other operand.
+template <class FORM, bool PLANES, bool IS_P, bool DOWN>
 struct RingStream {
     static constexpr int kLoads = IS_P ? FORM::kLoadsP : FORM::kLoadsQ, kBack = 4096;      // (offsets stay positive)
+    static constexpr int kEntries = IS_P ? FORM::kP : FORM::kQ, kChunks = kEntries / 8, kRows = 64 / kChunks;      // DOWN: 16-byte chunks of a row, rows of a load
     int unit, left, end, product, rows_in;
     const uint8_t *src, *src_s;
-    uint32_t off[kLoads], off_s;
-    int64_t step_s;
+    uint32_t off[kLoads], off_s, limit;
+    int64_t step, rest, step_s;      // DOWN: bytes from a K-tile to the next, from its first byte to the last chunk of the matrix
+
+    // 16-byte chunk c of row k at chunk c ^ turned(k), so that four rows of 64 bytes read together lie in different banks
+    static __device__ __forceinline__ int turned(int k) { return kChunks >= 16 ? (k & 3) << 2 : (k >> 1 & 1) << 2; }
 
     // parts multiplied, of P and of Q: (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
     static __device__ __forceinline__ int part(int product) { return ((IS_P ? 0x850 : 0x244) >> (2 * product)) & 3; }
@@ -194,6 +202,7 @@ struct RingStream {
     struct Place {
         const uint8_t *src;
         int left, product;
+        int64_t rest;
     };
     __device__ __forceinline__ void start(const RingJob &job, int wave, int lane) { go(of_unit(job, wave, lane)); }
     __device__ __forceinline__ void go(const Place &to)
@@ -201,6 +210,18 @@ struct RingStream {
         src = to.src;
         left = to.left;
         product = to.product;
+        rest = to.rest;
+        bound();
+    }
+    __device__ __forceinline__ void bound()
+    {
+        if (DOWN) limit = (uint32_t)min(rest, (int64_t)0x7fffffff) + kBack;
+    }
+    __device__ __forceinline__ void advance()
+    {
+        src += DOWN ? step : (int64_t)kRingRow;
+        if (DOWN) rest -= step;
+        bound();
     }
     __device__ __forceinline__ Place of_unit(const RingJob &job, int wave, int lane)
     {
@@ -210,14 +231,18 @@ struct RingStream {
         end = min(kt + job.k_per, job.nk);
         const int product = PLANES ? kt / job.plane_nk : 0, in_plane = PLANES ? kt - product * job.plane_nk : kt;
         const int left = PLANES ? min(job.plane_nk - in_plane, end - kt) : end - kt;
-        const uint8_t *const src = (IS_P ? job.P : job.Q) + (int64_t)row0 * ld + (int64_t)in_plane * kRingRow + (PLANES ? part(product) * (IS_P ? job.plane_p : job.plane_q) : 0) - kBack;
-        const int most = min(rows - 1 - row0, (IS_P ? FORM::kP : FORM::kQ) - 1);
+        step = 64 * ld;
+        const int64_t at = DOWN ? (int64_t)row0 * 2 + in_plane * step : (int64_t)row0 * ld + (int64_t)in_plane * kRingRow;
+        const int64_t rest = DOWN ? (IS_P ? job.downP : job.downQ) * ld - 16 - at : 0;
+        const uint8_t *const src = (IS_P ? job.P : job.Q) + at + (PLANES ? part(product) * (IS_P ? job.plane_p : job.plane_q) : 0) - kBack;
+        const int most = DOWN ? 0 : min(rows - 1 - row0, kEntries - 1);
         if (most != rows_in) {
             rows_in = most;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {      // load i fills LDS rows 8 n ... 8 n + 7, chunk c of a row at c ^ (row / 2); rows beyond the matrix: its last one again, whose results nobody stores
-                const int n = wave * kLoads + i;
-                off[i] = (uint32_t)min(n * 8 + (lane >> 3), most) * (uint32_t)ld + (uint32_t)((lane & 7) ^ ((4 * n + (lane >> 4)) & 7)) * 16 + kBack - (i & 3) * 1024;
+                const int n = wave * kLoads + i, k = n * kRows + lane / kChunks;
+                if (DOWN) off[i] = (uint32_t)k * (uint32_t)ld + (uint32_t)(lane % kChunks ^ turned(k)) * 16 + kBack - (i & 3) * 1024;
+                else off[i] = (uint32_t)min(n * 8 + (lane >> 3), most) * (uint32_t)ld + (uint32_t)((lane & 7) ^ ((4 * n + (lane >> 4)) & 7)) * 16 + kBack - (i & 3) * 1024;
             }
         }
         if (FORM::SCALES && !IS_P) {      // four bytes a lane; half of the waves load those of Q, the others those of P
@@ -228,7 +253,7 @@ struct RingStream {
             off_s = (uint32_t)min((int64_t)lane * 4, pitch - 4 - at);
             step_s = pitch;
         }
-        return {src, left, product};
+        return {src, left, product, rest};
     }
     __device__ __forceinline__ Place of_next(const RingJob &job, int each, int last, int wave, int lane)
     {
@@ -236,7 +261,8 @@ struct RingStream {
             const int next = (product + 1) * job.plane_nk;
             if (next < end) {
                 const int64_t parts = part(product + 1) - part(product);
-                return {src + parts * (IS_P ? job.plane_p : job.plane_q) - (int64_t)job.plane_nk * kRingRow, min(job.plane_nk, end - next), product + 1};
+                const int64_t back = job.plane_nk * (DOWN ? step : (int64_t)kRingRow);
+                return {src + parts * (IS_P ? job.plane_p : job.plane_q) - back, min(job.plane_nk, end - next), product + 1, rest + back};
             }
         }
         unit = min(unit + each, last);      // (past the last unit: the last one again, which nobody reads)
@@ -249,7 +275,8 @@ struct RingStream {
     __device__ __forceinline__ void issue(uint8_t *slot, int wave) const
     {
         if constexpr (FROM < TO) {
-            __builtin_amdgcn_global_load_lds((gptr_t)(src + off[FROM]), (lptr_t)(slot + wave * kLoads * 1024 + (FROM & ~3) * 1024), 16, (FROM & 3) * 1024, 0);
+            const uint32_t at = DOWN ? min(off[FROM], limit - (FROM & 3) * 1024) : off[FROM];
+            __builtin_amdgcn_global_load_lds((gptr_t)(src + at), (lptr_t)(slot + wave * kLoads * 1024 + (FROM & ~3) * 1024), 16, (FROM & 3) * 1024, 0);
             issue<FROM + 1, TO>(slot, wave);
         }
     }
@@ -299,8 +326,21 @@ __device__ __forceinline__ void results_ready(v16f (&acc)[FORM::TP][FORM::TQ])
     }
 }
 
+// A fragment of 32 entries and 16 k of an operand [k][entries]: eight k of one entry for a lane.  A group of 16 lanes reads four k of 16 entries, and each lane gets one entry's.
+// (__restrict__ is what tells the compiler that these reads are not of what the loads on their way write; without it every one waited for all of them, and a product took half as long again.)
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef s16x4 __attribute__((address_space(3))) *down_t;
+template <int ENTRIES>
+__device__ __forceinline__ bf16x8 read_down(const uint8_t *__restrict__ at, int ks)
+{
+    union { s16x4 h[2]; bf16x8 all; } v;
+    v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((down_t)(at + ks * 16 * ENTRIES * 2));
+    v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((down_t)(at + (ks * 16 + 4) * ENTRIES * 2));
+    return v.all;
+}
+
 // epilogue(acc, p0, q0, split, staging, lane): first entries of the wave's part of a tile; stores at least EPILOGUE::kStores times for a wave or waits for its stores.
-template <class FORM, class OP, bool PLANES, class EPILOGUE>
+template <class FORM, class OP, bool PLANES, bool DOWN_P, bool DOWN_Q, class EPILOGUE>
 __device__ __forceinline__ void ring(const RingCall<EPILOGUE> &call)
 {
     const RingJob &job = call.job;
@@ -314,8 +354,10 @@ __device__ __forceinline__ void ring(const RingCall<EPILOGUE> &call)
     const int first = xcd * share + ((int)blockIdx.x >> 3), end = min(total, (xcd + 1) * share);
     if (first >= end) return;
 
-    RingStream<FORM, PLANES, true> from_p;
-    RingStream<FORM, PLANES, false> from_q;
+    typedef RingStream<FORM, PLANES, true, DOWN_P> FromP;
+    typedef RingStream<FORM, PLANES, false, DOWN_Q> FromQ;
+    FromP from_p;
+    FromQ from_q;
     from_p.unit = from_q.unit = first;
     from_p.rows_in = from_q.rows_in = -1;
     from_p.start(job, wave, lane);
@@ -326,6 +368,14 @@ __device__ __forceinline__ void ring(const RingCall<EPILOGUE> &call)
 #pragma unroll
     for (int c = 0; c < 4; ++c) chunk[c] = row * kRingRow + (((2 * c + half) ^ (row >> 1)) & 7) * 16;
 
+    // DOWN: where a lane of a 16 x 16 transposing read starts in the first step's rows of a fragment
+    int down_p[TP], down_q[TQ];
+    const int down_k = half * 8 + ((lane & 15) >> 2), in_tile = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+#pragma unroll
+    for (int i = 0; i < TP; ++i) down_p[i] = down_k * FORM::kP * 2 + ((((wp * TP + i) * 4 + in_tile) ^ FromP::turned(down_k)) << 4) + (lane & 1) * 8;
+#pragma unroll
+    for (int j = 0; j < TQ; ++j) down_q[j] = down_k * FORM::kQ * 2 + ((((wq * TQ + j) * 4 + in_tile) ^ FromQ::turned(down_k)) << 4) + (lane & 1) * 8;
+
     v16f acc[TP][TQ];
     typename OP::Frag fp[2][TP], fq[2][TQ];
     int sp[2][TP], sq[2][TQ];
@@ -334,9 +384,15 @@ __device__ __forceinline__ void ring(const RingCall<EPILOGUE> &call)
         constexpr int S = decltype(set_c)::value;
         const uint8_t *const p = ring_lds + at_p + wp * TP * 32 * kRingRow, *const q = ring_lds + FORM::kAtQ + at_q + wq * TQ * 32 * kRingRow;
 #pragma unroll
-        for (int i = 0; i < TP; ++i) fp[S][i] = OP::read(p + i * 32 * kRingRow, chunk, ks);
+        for (int i = 0; i < TP; ++i) {
+            if constexpr (DOWN_P) fp[S][i] = read_down<FORM::kP>(ring_lds + at_p + down_p[i], ks);
+            else fp[S][i] = OP::read(p + i * 32 * kRingRow, chunk, ks);
+        }
 #pragma unroll
-        for (int j = 0; j < TQ; ++j) fq[S][j] = OP::read(q + j * 32 * kRingRow, chunk, ks);
+        for (int j = 0; j < TQ; ++j) {
+            if constexpr (DOWN_Q) fq[S][j] = read_down<FORM::kQ>(ring_lds + FORM::kAtQ + at_q + down_q[j], ks);
+            else fq[S][j] = OP::read(q + j * 32 * kRingRow, chunk, ks);
+        }
         if (FORM::SCALES) {
             const uint8_t *const scales = ring_lds + FORM::kAtS + at_s;
 #pragma unroll
@@ -357,7 +413,7 @@ __device__ __forceinline__ void ring(const RingCall<EPILOGUE> &call)
     int free_p = 0, free_q = 0, free_s = 0;      // the slots that the next loads fill
     auto loaded_p = [&]() {
         free_p = free_p == (FORM::NP - 1) * FORM::kSlotP ? 0 : free_p + FORM::kSlotP;
-        from_p.src += kRingRow;
+        from_p.advance();
         __builtin_amdgcn_sched_barrier(0);
         if (--from_p.left == 0) from_p.change(again(call).job, each, total - 1, wave, lane);
     };
@@ -368,7 +424,7 @@ __device__ __forceinline__ void ring(const RingCall<EPILOGUE> &call)
     auto loaded_q = [&]() {
         free_q = free_q == (FORM::NQ - 1) * FORM::kSlotQ ? 0 : free_q + FORM::kSlotQ;
         if (FORM::SCALES) free_s = free_s == (FORM::NQ - 1) * FORM::kSlotS ? 0 : free_s + FORM::kSlotS;
-        from_q.src += kRingRow;
+        from_q.advance();
         __builtin_amdgcn_sched_barrier(0);
         if (--from_q.left == 0) from_q.change(again(call).job, each, total - 1, wave, lane);
     };
@@ -392,7 +448,7 @@ __device__ __forceinline__ void ring(const RingCall<EPILOGUE> &call)
     };
     // Nothing else fills a SIMD's matrix cores while its only wave reads or loads, so reads and loads go between the products, and the products of a step stay on their side
     // of the barrier (left to itself the compiler gathers the reads before the wait and the products behind it).
-    constexpr int kFragments = (TP + TQ) * OP::kReads + (FORM::SCALES ? TP + TQ : 0), kProducts = TP * TQ * OP::kPerPair;
+    constexpr int kFragments = TP * (DOWN_P ? 2 : OP::kReads) + TQ * (DOWN_Q ? 2 : OP::kReads) + (FORM::SCALES ? TP + TQ : 0), kProducts = TP * TQ * OP::kPerPair;
     auto step = [&](auto first_c) {      // a K-tile, the first one of a tile or a later one
         typedef decltype(first_c) First;
         auto inner = [&](auto r_c) {

@@ -1,11 +1,13 @@
 """Builds libcdl.so (the HIP kernels and the C boundary) for gfx950 with hipcc and the Python calls to it, in-tree."""
 from __future__ import annotations
 
+import concurrent.futures
 import glob
 import hashlib
 import os
 import subprocess
 import sysconfig
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
@@ -25,6 +27,10 @@ HIPCC_FLAGS = [
     "-ffp-contract=off",
     "-Wall", "-Wno-unused-command-line-argument",
 ]
+
+
+# the ones that take longest to compile, whatever their size: many forms of one loop
+LONG_COMPILES = ("cdl_block8_gemm.hip", "cdl_head_loss.hip")
 
 
 def sources():
@@ -78,14 +84,23 @@ def build_lib(verbose: bool = False) -> str:
     """Compile every .hip source into libcdl.so (always recompiles)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp = LIB_PATH + ".tmp.%d" % os.getpid()
-    cmd = [hipcc] + HIPCC_FLAGS + ["-I", os.path.join(_ROOT, "include"), "-I", CSRC] + sources() + ["-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + res.stdout)
-    if verbose and res.stdout.strip():
-        print(res.stdout)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + res.stdout)
+        if verbose and res.stdout.strip():
+            print(res.stdout)
+
+    # the sources side by side (one behind the other they take minutes), the largest first, then one link
+    with tempfile.TemporaryDirectory() as objects, concurrent.futures.ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        compile_flags = [flag for flag in HIPCC_FLAGS if flag != "-shared"]
+        largest_first = sorted(sources(), key=lambda source: (os.path.basename(source) not in LONG_COMPILES, -os.path.getsize(source)))
+        objs = {source: os.path.join(objects, os.path.basename(source) + ".o") for source in sources()}
+        list(pool.map(lambda source: run([hipcc] + compile_flags + ["-I", os.path.join(_ROOT, "include"), "-I", CSRC, "-c", source, "-o", objs[source]]), largest_first))
+        run([hipcc] + HIPCC_FLAGS + list(objs.values()) + ["-o", tmp])
     build_marshal()
     os.replace(tmp, LIB_PATH)
     if LIB_PATH.endswith(os.path.join(os.path.basename(_HERE), "libcdl.so")):

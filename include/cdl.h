@@ -438,6 +438,8 @@ int cdl_block8_gemm(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, 
  * vocabulary): h[T,D] hidden states, w[V,D] the layer's weights, both of `type`, z = h . w^T never in memory as a whole.
  *   lse[t]  = log sum_v exp(z[t,v])                                  (fp32[T], required)
  *   loss[t] = lse[t] - z[t, target[t]]                               (fp32[T], nullable)
+ * A logit of -infinity has no share in the sum (all of them: lse -infinity), one of +infinity makes it infinite; so do logits beyond 2^127.  (fp32: logits of infinite
+ * operands are NaN.)
  * target: int64[T].  A token whose target lies outside [0, V) is padding: loss 0; its lse is formed.  Nothing that a
  * padding token holds reaches any other token, unless it is not finite (0 times infinity in d_w).
  *

@@ -66,7 +66,8 @@ struct Reduce {
                 for (int r = 0; r < 16; ++r) m = fmaxf(m, value(i, r));
             asm volatile("" : "+v"(end));
             m = fmaxf(m, __shfl_xor(m, 32, 64));
-            const float shift = -m * kLog2e;
+            // (logits from 2^127 on count as infinite: a stretch of none but -infinity adds nothing, one with +infinity makes the sum infinite; less m they would be no numbers)
+            const float shift = fabsf(m) < 0x1p127f ? -m * kLog2e : 0.0f;
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll

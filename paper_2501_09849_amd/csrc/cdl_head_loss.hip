@@ -138,7 +138,9 @@ void head_finish_kernel(const float2 *__restrict__ partial, int stretches, const
 
 // ---- operands -------------------------------------------------------------------------------------------------------
 
-// x[rows, D] as bf16 rows of Dp entries, zeros beyond D; fp32 in three parts [3][rows][Dp] whose sum is x: each the rest rounded to bf16.
+// x[rows, D] as bf16 rows of Dp entries, zeros beyond D; fp32 in three parts [3][rows][Dp] whose sum is x: each the rest rounded to bf16, the first one of a finite entry the
+// largest finite bf16 where rounding would give infinity (the rest of it would be infinite too, and their products no numbers).
+constexpr float kLargest = 0x1.fep127f;
 template <class T>
 __global__ __launch_bounds__(256)
 void head_rows_kernel(const T *__restrict__ x, int64_t rows, int D, int Dp, bf16_t *__restrict__ out)
@@ -157,15 +159,23 @@ void head_rows_kernel(const T *__restrict__ x, int64_t rows, int D, int Dp, bf16
         for (int k = 0; k < 8; ++k) v[k] = d + k < D ? (float)at[k] : 0.0f;
     }
     bf16_t *to = out + r * Dp + d;
-    store8(to, v, false);
     if constexpr (sizeof(T) == 4) {
+        float part[8];
 #pragma unroll
-        for (int part = 1; part < 3; ++part) {
+        for (int k = 0; k < 8; ++k) part[k] = fabsf(v[k]) < INFINITY ? fminf(fmaxf(v[k], -kLargest), kLargest) : v[k];
+        store8(to, part, false);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] -= (float)(bf16_t)v[k];
+        for (int i = 1; i < 3; ++i) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] -= (float)(bf16_t)part[k];
+                part[k] = v[k];
+            }
             to += rows * Dp;
-            store8(to, v, false);
+            store8(to, part, false);
         }
+    } else {
+        store8(to, v, false);
     }
 }
 

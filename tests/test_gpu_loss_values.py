@@ -1,4 +1,4 @@
-"""The loss of the last layer where logits are infinite or the lowest."""
+"""The loss of the last layer where logits are infinite or the lowest, and where weights are the largest."""
 import pytest
 
 import gpu_util as gu
@@ -89,3 +89,22 @@ def test_logits_that_are_all_infinite(env, T, V, D):
     loss, lse = case.forward()
     assert float(lse[0]) == float("-inf") and float(lse[1]) == float("inf") and float(loss[1]) == float("inf")
     assert torch.equal(lse[2:], plain[1][2:]) and torch.equal(loss[3:], plain[0][3:]) and torch.isfinite(plain[1]).all()      # (the features that differ are zero there)
+
+
+def test_fp32_weights_up_to_the_largest(env):
+    """An fp32 operand is used as three bf16 parts: also one that rounds to infinity as bf16."""
+    torch, _ = env
+    T, V, D = 40, 300, 64
+    top = torch.finfo(torch.float32).max
+    case = Case(env, T, V, D, "float32", padding=0.0)
+    case.h[:, 0] = 2.0 ** -127 * torch.randint(2, 64, (T,), device="cuda").float()      # two logits up to 126
+    case.w[7, 0], case.w[8, 0] = top, -top
+    ok = torch.ones(T, dtype=torch.bool, device="cuda")
+    every = torch.arange(V, device="cuda")
+    case.d_lse = torch.zeros(T, device="cuda")
+    loss, lse, _, d_w, error = formulas(torch, case, every, ok)
+    got_loss, got_lse = case.forward()
+    # (h's entry is 2^-126 to 2^-122, whose parts below 2^-126 the matrix cores take as zero; it has six bits, so one part holds it)
+    assert ((got_lse.double() - lse).abs() <= error).all() and ((got_loss.double() - loss).abs() <= error).all()
+    got_w = case.backward(got_lse, want_h=False)[1]
+    assert float((got_w.double() - d_w)[:, 1:].norm()) <= 2e-5 * float(d_w[:, 1:].norm())

@@ -245,7 +245,8 @@ struct Gradient {
         if (!PARTS) return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -lse));      // (lse times log2 e)
         // the rounding of the product with log2 e goes into a second factor
         const float e = z - lse, hi = e * kLog2e, lo = __builtin_fmaf(e, kLog2e, -hi) + e * 1.925963033500703e-8f, x = __builtin_amdgcn_exp2f(hi);
-        return e > -INFINITY ? __builtin_fmaf(x, lo * 0.69314718055994530942f, x) : 0.0f;
+        // (exp(-150) is below half of the smallest float; further down hi and lo become infinite.  NaN is not below.)
+        return e < -150.0f ? 0.0f : __builtin_fmaf(x, lo * 0.69314718055994530942f, x);
     }
     __device__ __forceinline__ void operator()(const v16f (&acc)[FORM::TP][FORM::TQ], int p0, int q0, int, uint8_t *staging, int lane) const
     {

@@ -1,4 +1,4 @@
-"""The loss of the last layer where logits are infinite or the lowest, and where weights are the largest."""
+"""The loss of the last layer where logits are infinite, the lowest or no numbers, and where weights are the largest."""
 import pytest
 
 import gpu_util as gu
@@ -47,7 +47,7 @@ def formulas(torch, case, kept, ok):
 
 
 @pytest.mark.parametrize("T,V,D", SIZES)
-@pytest.mark.parametrize("type_", ["bfloat16"])
+@pytest.mark.parametrize("type_", ["bfloat16", "float32"])
 def test_words_of_the_lowest_weight(env, T, V, D, type_):
     """A vocabulary padded with words whose only weight is the type's lowest value: no share in the log-sum, no gradient."""
     torch, _ = env
@@ -89,6 +89,25 @@ def test_logits_that_are_all_infinite(env, T, V, D):
     loss, lse = case.forward()
     assert float(lse[0]) == float("-inf") and float(lse[1]) == float("inf") and float(loss[1]) == float("inf")
     assert torch.equal(lse[2:], plain[1][2:]) and torch.equal(loss[3:], plain[0][3:]) and torch.isfinite(plain[1]).all()      # (the features that differ are zero there)
+
+
+@pytest.mark.parametrize("type_", ["bfloat16", "float32"])
+def test_no_numbers_are_never_hidden(env, type_):
+    """A token with NaN: its loss, its d_h and all of d_w; a word with NaN: every token's loss and every gradient."""
+    torch, _ = env
+    T, V, D = 70, 300, 64
+    case = Case(env, T, V, D, type_, padding=0.0)
+    case.h[17, 3] = float("nan")
+    loss, lse = case.forward()
+    d_h, d_w = case.backward(lse)
+    rest = torch.arange(T, device="cuda") != 17
+    assert torch.isnan(loss[17]) and torch.isnan(lse[17]) and torch.isfinite(lse[rest]).all()
+    assert torch.isnan(d_h[17]).all() and torch.isfinite(d_h[rest].float()).all() and torch.isnan(d_w).all()
+    case = Case(env, T, V, D, type_, padding=0.0)
+    case.w[40, 5] = float("nan")
+    loss, lse = case.forward()
+    d_h, d_w = case.backward(lse)
+    assert torch.isnan(loss).all() and torch.isnan(lse).all() and torch.isnan(d_h).all() and torch.isnan(d_w).all()
 
 
 def test_fp32_weights_up_to_the_largest(env):

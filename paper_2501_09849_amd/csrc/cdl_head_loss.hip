@@ -11,7 +11,9 @@
 namespace cdl {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr double kLog2eWhole = 1.44269504088896340736;
+constexpr float kLog2e = (float)kLog2eWhole, kLog2eRest = (float)(kLog2eWhole - (double)kLog2e);      // log2 e as the sum of two floats
+constexpr float kLn2 = 0.69314718055994530942f;
 
 using Wide = RingForm<2, 2, 4, 4, 3, 2, 1>;        // 256 x 256
 using Square = RingForm<2, 2, 2, 2, 3, 2, 2>;      // 128 x 128
@@ -243,10 +245,10 @@ struct Gradient {
     __device__ __forceinline__ static float probability(float z, float lse)
     {
         if (!PARTS) return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -lse));      // (lse times log2 e)
-        // the rounding of the product with log2 e goes into a second factor
-        const float e = z - lse, hi = e * kLog2e, lo = __builtin_fmaf(e, kLog2e, -hi) + e * 1.925963033500703e-8f, x = __builtin_amdgcn_exp2f(hi);
+        // exp(e) = 2^hi 2^lo, hi the rounded product with log2 e and lo what it leaves: 2^lo = 1 + lo ln 2, as lo is below 2^-16
+        const float e = z - lse, hi = e * kLog2e, lo = __builtin_fmaf(e, kLog2e, -hi) + e * kLog2eRest, x = __builtin_amdgcn_exp2f(hi);
         // (exp(-150) is below half of the smallest float; further down hi and lo become infinite.  NaN is not below.)
-        return e < -150.0f ? 0.0f : __builtin_fmaf(x, lo * 0.69314718055994530942f, x);
+        return e < -150.0f ? 0.0f : __builtin_fmaf(x, lo * kLn2, x);
     }
     __device__ __forceinline__ void operator()(const v16f (&acc)[FORM::TP][FORM::TQ], int p0, int q0, int, uint8_t *staging, int lane) const
     {

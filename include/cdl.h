@@ -409,6 +409,7 @@ int64_t cdl_block8_pitch(int32_t n);
  *           down the columns of x: the operands of the backward products.  With tiles the values are those of q.
  * pitch(n) = cdl_block8_pitch(n).  Either pair (q, scale) or (q_t, scale_t) may be NULL, not
  * both.  A block with an entry that is not finite gets scale 255 and its products come out NaN.  x 16-byte aligned, as are the outputs.
+ * CDL_ERR_RANGE for 2^24 blocks of 128 x 128 or more.
  */
 int cdl_block8_quantize(const void *x, int32_t type, int32_t rows, int32_t cols, int32_t tiles, int32_t format,
                         uint8_t *q, uint8_t *scale, uint8_t *q_t, uint8_t *scale_t, void *hip_stream);

@@ -208,7 +208,7 @@ int launch_block8_quantize(const void *x, int32_t type, int32_t rows, int32_t co
 {
     const int64_t pc = block8_pitch(cols), pr = block8_pitch(rows), blocks = (pc / 128) * (pr / 128);
     if (blocks == 0) return CDL_OK;
-    if (blocks > INT32_MAX) return CDL_ERR_RANGE;
+    if (blocks * kThreads >= 1ll << 32) return CDL_ERR_RANGE;
     const QuantArgs a{x, rows, cols, (int)(pc / 128), pc, pr, q, scale, q_t, scale_t};
     return type == CDL_BF16 ? launch<bf16_t>(a, tiles != 0, format == CDL_E5M2, blocks, stream) : launch<float>(a, tiles != 0, format == CDL_E5M2, blocks, stream);
 }

@@ -150,10 +150,11 @@ int launch_block8_gemm(const uint8_t *a, const uint8_t *a_scale, const uint8_t *
     const int64_t n = (int64_t)M * N;
     if (n == 0) return CDL_OK;
     if (K == 0) {
-        const unsigned blocks = (unsigned)((n + 255) / 256);
-        if (y_type == CDL_BF16) CDL_LAUNCH("block8_zero_kernel", stream, zero_kernel<bf16_t>, dim3(blocks), dim3(256), 0, (bf16_t *)y, n);
-        else CDL_LAUNCH("block8_zero_kernel", stream, zero_kernel<float>, dim3(blocks), dim3(256), 0, (float *)y, n);
-        return check_launch();
+        return in_launches(n, kLaunchThreads, [&](int64_t at, int64_t count) {
+            const unsigned blocks = (unsigned)((count + 255) / 256);
+            if (y_type == CDL_BF16) CDL_LAUNCH("block8_zero_kernel", stream, zero_kernel<bf16_t>, dim3(blocks), dim3(256), 0, (bf16_t *)y + at, count);
+            else CDL_LAUNCH("block8_zero_kernel", stream, zero_kernel<float>, dim3(blocks), dim3(256), 0, (float *)y + at, count);
+        });
     }
     const Layout l = layout(M, N, K);
     const int64_t ld = block8_pitch(K);

@@ -66,12 +66,13 @@ template <class T>
 int launch(const void *x, const void *add, int64_t n, uint32_t share, uint64_t seed, uint64_t counter, void *y, hipStream_t stream)
 {
     const float scale = share < 65536 ? 65536.0f / (float)(65536 - share) : 0.0f;
-    const int64_t blocks = ((n + 7) / 8 + kThreads - 1) / kThreads;
     const bool past = n * (int64_t)sizeof(T) >= kStreamFrom * 4;
     const auto kernel = add ? dropout_kernel<T, true> : dropout_kernel<T, false>;
-    CDL_LAUNCH("dropout_kernel", stream, kernel, dim3((unsigned)blocks), dim3(kThreads), 0, (const T *)x, (const T *)add, (T *)y, n, share, scale,
-               seed, counter, past);
-    return check_launch();
+    return in_launches(n, 8 * kLaunchThreads, [&](int64_t at, int64_t count) {
+        const int64_t blocks = ((count + 7) / 8 + kThreads - 1) / kThreads;
+        CDL_LAUNCH("dropout_kernel", stream, kernel, dim3((unsigned)blocks), dim3(kThreads), 0, (const T *)x + at, add ? (const T *)add + at : nullptr, (T *)y + at, count, share,
+                   scale, seed, counter + (uint64_t)at / 8, past);
+    });
 }
 
 }  // namespace

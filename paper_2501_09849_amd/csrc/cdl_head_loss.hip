@@ -140,12 +140,12 @@ void head_finish_kernel(const float2 *__restrict__ partial, int stretches, const
 
 // ---- operands -------------------------------------------------------------------------------------------------------
 
-// x[rows, D] as bf16 rows of Dp entries, zeros beyond D; fp32 in three parts [3][rows][Dp] whose sum is x: each the rest rounded to bf16, the first one of a finite entry the
+// x[rows, D] as bf16 rows of Dp entries, zeros beyond D; fp32 in three parts [rows][Dp], plane entries apart, whose sum is x: each the rest rounded to bf16, the first one of a finite entry the
 // largest finite bf16 where rounding would give infinity (the rest of it would be infinite too, and their products no numbers).
 constexpr float kLargest = 0x1.fep127f;
 template <class T>
 __global__ __launch_bounds__(256)
-void head_rows_kernel(const T *__restrict__ x, int64_t rows, int D, int Dp, bf16_t *__restrict__ out)
+void head_rows_kernel(const T *__restrict__ x, int64_t rows, int64_t plane, int D, int Dp, bf16_t *__restrict__ out)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;      // eight entries
     const int per = Dp / 8;
@@ -173,7 +173,7 @@ void head_rows_kernel(const T *__restrict__ x, int64_t rows, int D, int Dp, bf16
                 v[k] -= (float)(bf16_t)part[k];
                 part[k] = v[k];
             }
-            to += rows * Dp;
+            to += plane;
             store8(to, part, false);
         }
     } else {
@@ -336,12 +336,12 @@ void head_product_kernel(RingCall<Store<FORM, T, ADD>> call)
 
 template <class T>
 __global__ __launch_bounds__(256)
-void head_sum_kernel(const float *__restrict__ parts, int splits, int64_t n, const float *__restrict__ by, T *__restrict__ y)
+void head_sum_kernel(const float *__restrict__ parts, int splits, int64_t part, int64_t n, const float *__restrict__ by, T *__restrict__ y)
 {
     const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (e >= n) return;
     float sum = 0.0f;
-    for (int s = 0; s < splits; ++s) sum += parts[s * n + e];
+    for (int s = 0; s < splits; ++s) sum += parts[s * part + e];
     y[e] = (T)(sum * *by);
 }
 
@@ -512,8 +512,9 @@ int run_product(Form form, const RingJob &job, const RowTarget<T> &to, int64_t p
 template <class T>
 int to_rows(const T *x, int64_t rows, int64_t D, int64_t Dp, bf16_t *out, hipStream_t stream)
 {
-    CDL_LAUNCH("head_rows_kernel", stream, head_rows_kernel<T>, dim3(blocks_of(rows * (Dp / 8), 256)), dim3(256), 0, x, rows, (int)D, (int)Dp, out);
-    return check_launch();
+    return in_launches(rows, kLaunchThreads / (Dp / 8), [&](int64_t at, int64_t count) {
+        CDL_LAUNCH("head_rows_kernel", stream, head_rows_kernel<T>, dim3(blocks_of(count * (Dp / 8), 256)), dim3(256), 0, x + at * D, count, rows * Dp, (int)D, (int)Dp, out + at * Dp);
+    });
 }
 
 template <class T>
@@ -586,7 +587,10 @@ int backward(const T *h, const T *w, int32_t type, const int64_t *target, const 
     }
     if (d_h) {
         const int64_t n = (int64_t)tokens * D;
-        CDL_LAUNCH("head_sum_kernel", stream, head_sum_kernel<T>, dim3(blocks_of(n, 256)), dim3(256), 0, (const float *)sums, p.split_h.splits, n, (const float *)unit, d_h);
+        CDL_TRY(in_launches(n, kLaunchThreads, [&](int64_t at, int64_t count) {
+            CDL_LAUNCH("head_sum_kernel", stream, head_sum_kernel<T>, dim3(blocks_of(count, 256)), dim3(256), 0, (const float *)sums + at, p.split_h.splits, n, count,
+                       (const float *)unit, d_h + at);
+        }));
     }
     return check_launch();
 }
@@ -595,8 +599,9 @@ template <class T>
 int zero(T *y, int64_t n, hipStream_t stream)
 {
     if (!y || n == 0) return CDL_OK;
-    CDL_LAUNCH("head_zero_kernel", stream, head_zero_kernel<T>, dim3(blocks_of(n, 256)), dim3(256), 0, y, n);
-    return check_launch();
+    return in_launches(n, kLaunchThreads, [&](int64_t at, int64_t count) {
+        CDL_LAUNCH("head_zero_kernel", stream, head_zero_kernel<T>, dim3(blocks_of(count, 256)), dim3(256), 0, y + at, count);
+    });
 }
 
 }  // namespace

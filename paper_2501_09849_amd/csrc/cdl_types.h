@@ -13,6 +13,19 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// A grid holds fewer than 2^32 threads: what has more entries than that goes through in several launches, launch(first, count) for kLaunchThreads at a time.
+constexpr int64_t kLaunchThreads = 1ll << 31;
+template <class F>
+int in_launches(int64_t n, int64_t most, const F &launch)
+{
+    for (int64_t at = 0; at < n; at += most) {
+        launch(at, n - at < most ? n - at : most);
+        const int rc = check_launch();
+        if (rc != CDL_OK) return rc;
+    }
+    return CDL_OK;
+}
+
 // Eight consecutive entries from 16-byte aligned memory (fp32: two loads), as fp32; past the caches if `stream`.
 __device__ __forceinline__ void load8(const float *p, float (&v)[8], bool stream)
 {

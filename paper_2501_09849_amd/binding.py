@@ -353,32 +353,39 @@ def cdl_qconv_fwd(x_idx, w_idx, B, H, W, C, N, R, S, stride, pad, delta_x, delta
            "cdl_qconv_fwd")
 
 
-_TYPES = {"torch.float32": F32, "torch.bfloat16": BF16}
-_TYPE_OF = {}             # the same by dtype, filled as they are met
+class _Fit(dict):
+    """The dtypes that fit an argument, by name; looked up once each.  Tensors of other types would be read or written beyond their ends, or as other numbers."""
+
+    def __init__(self, *names):
+        super().__init__()
+        self.names = names
+
+    def __missing__(self, dtype):
+        if str(dtype) not in self.names:
+            raise TypeError("a tensor of %s is needed, got %s" % (" or ".join(self.names), dtype))
+        self[dtype] = True
+        return True
 
 
-def _type_of(t, given=None) -> int:
-    """F32 or BF16: what is given, or the tensor's own (an address has none)."""
-    if given is not None:
-        return given
+_TYPES = {F32: _Fit("torch.float32"), BF16: _Fit("torch.bfloat16")}
+_FLOATS, _INDICES = _TYPES[F32], _Fit("torch.int64")
+_VALUES = {E4M3: _Fit("torch.uint8", "torch.int8", "torch.float8_e4m3fn"), E5M2: _Fit("torch.uint8", "torch.int8", "torch.float8_e5m2")}
+_SCALES = _Fit("torch.uint8", "torch.int8", "torch.float8_e8m0fnu")
+_TYPE_OF = {}             # F32 or BF16 by dtype, filled as they are met
+
+
+def _type_of(t, given) -> int:
+    """F32 or BF16: the tensor's own, or for an address what is given."""
     dtype = getattr(t, "dtype", None)
-    kind = _TYPE_OF.get(dtype)
+    kind = given if dtype is None else _TYPE_OF.get(dtype)
     if kind is None:
-        kind = _TYPES.get(str(dtype))
+        kind = {"torch.float32": F32, "torch.bfloat16": BF16}.get(str(dtype))
         if kind is None:
             raise TypeError("a float32 or bfloat16 tensor, or the type of an address, is needed: got %s" % (dtype,))
         _TYPE_OF[dtype] = kind
+    if given is not None and given != kind:
+        raise TypeError("a tensor of %s is not of type %s" % (dtype, given))
     return kind
-
-
-def _same_type(what, first, *others) -> None:
-    """Tensors of another type than the first would be read or written beyond their ends.  Addresses and None have none."""
-    like = getattr(first, "dtype", None)
-    if like is not None:
-        for t in others:
-            dtype = getattr(t, "dtype", like)
-            if dtype is not like:
-                raise TypeError("%s: %s tensors are needed, got %s" % (what, like, dtype))
 
 
 def block8_pitch(n: int) -> int:
@@ -386,8 +393,9 @@ def block8_pitch(n: int) -> int:
 
 
 def cdl_block8_quantize(x, rows, cols, q=None, scale=None, q_t=None, scale_t=None, tiles=False, format=E4M3, stream=None, type=None):
-    _check((_CALLS or _calls()).cdl_block8_quantize(x, _type_of(x, type), rows, cols, 1 if tiles else 0, format, q, scale, q_t, scale_t, stream),
-           "cdl_block8_quantize")
+    calls, values = _CALLS or _calls(), _VALUES.get(format, _SCALES)      # (a number that is no format is for the library to refuse)
+    calls.fit(values, q, values, q_t, _SCALES, scale, _SCALES, scale_t)
+    _check(calls.cdl_block8_quantize(x, _type_of(x, type), rows, cols, 1 if tiles else 0, format, q, scale, q_t, scale_t, stream), "cdl_block8_quantize")
 
 
 def block8_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -395,35 +403,33 @@ def block8_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
 
 
 def cdl_block8_gemm(a, a_scale, b, b_scale, M, N, K, y, ws=None, stream=None, a_format=E4M3, b_format=E4M3, y_type=None):
-    _check((_CALLS or _calls()).cdl_block8_gemm(a, a_scale, b, b_scale, M, N, K, a_format, b_format, y, _type_of(y, y_type), ws, stream),
-           "cdl_block8_gemm")
+    calls = _CALLS or _calls()
+    calls.fit(_VALUES.get(a_format, _SCALES), a, _VALUES.get(b_format, _SCALES), b, _SCALES, a_scale, _SCALES, b_scale)
+    _check(calls.cdl_block8_gemm(a, a_scale, b, b_scale, M, N, K, a_format, b_format, y, _type_of(y, y_type), ws, stream), "cdl_block8_gemm")
 
 
 def head_loss_workspace_bytes(T: int, V: int, D: int, type: int, train: bool = False) -> int:
     return int(load().cdl_head_loss_workspace_bytes(T, V, D, type, 1 if train else 0))
 
 
-def _index_type(target) -> None:
-    if str(getattr(target, "dtype", "torch.int64")) != "torch.int64":
-        raise TypeError("targets are int64: got %s" % (target.dtype,))
-
-
 def cdl_head_loss_fwd(h, w, target, T, V, D, loss, lse, ws=None, stream=None, type=None):
-    _same_type("cdl_head_loss_fwd", h, w)
-    _index_type(target)
-    _check((_CALLS or _calls()).cdl_head_loss_fwd(h, w, _type_of(h, type), target, T, V, D, loss, lse, ws, stream), "cdl_head_loss_fwd")
+    calls, kind = _CALLS or _calls(), _type_of(h, type)
+    calls.fit(_TYPES.get(kind, _FLOATS), w, _INDICES, target, _FLOATS, loss, _FLOATS, lse)
+    _check(calls.cdl_head_loss_fwd(h, w, kind, target, T, V, D, loss, lse, ws, stream), "cdl_head_loss_fwd")
 
 
 def cdl_head_loss_bwd(h, w, target, lse, T, V, D, d_h=None, d_w=None, ws=None, d_loss=None, d_lse=None, stream=None, type=None):
-    _same_type("cdl_head_loss_bwd", h, w, d_h, d_w)
-    _index_type(target)
-    _check((_CALLS or _calls()).cdl_head_loss_bwd(h, w, _type_of(h, type), target, lse, d_loss, d_lse, T, V, D, d_h, d_w, ws, stream),
-           "cdl_head_loss_bwd")
+    calls, kind = _CALLS or _calls(), _type_of(h, type)
+    like = _TYPES.get(kind, _FLOATS)
+    calls.fit(like, w, like, d_h, like, d_w, _INDICES, target, _FLOATS, lse, _FLOATS, d_loss, _FLOATS, d_lse)
+    _check(calls.cdl_head_loss_bwd(h, w, kind, target, lse, d_loss, d_lse, T, V, D, d_h, d_w, ws, stream), "cdl_head_loss_bwd")
 
 
 def cdl_dropout(x, n, p, seed, counter, y, add=None, stream=None, type=None):
-    _same_type("cdl_dropout", x, add, y)
-    _check((_CALLS or _calls()).cdl_dropout(x, add, _type_of(x, type), n, p, seed, counter, y, stream), "cdl_dropout")
+    calls, kind = _CALLS or _calls(), _type_of(x, type)
+    like = _TYPES.get(kind, _FLOATS)
+    calls.fit(like, add, like, y)
+    _check(calls.cdl_dropout(x, add, kind, n, p, seed, counter, y, stream), "cdl_dropout")
 
 
 def cdl_probe_mfma_int8(iters: int, random_operands: bool, blocks: int, sink, stream=None) -> float:

@@ -4,7 +4,7 @@
  * GPU time each, so what Python spends per call counts: 7 us with ctypes (two Python-level calls per tensor, a Stream
  * object, a struct, ctypes' own conversion of fifteen arguments), 1.5 us here.
  *
- * Tensors are used through their methods only (is_contiguous, data_ptr, nbytes); addresses of the library's functions
+ * Tensors are used through their methods only (is_contiguous, data_ptr, nbytes, dtype); addresses of the library's functions
  * come from the caller (init), which has loaded the library.
  */
 #define PY_SSIZE_T_CLEAN
@@ -14,7 +14,7 @@
 
 #include "cdl.h"
 
-static PyObject *s_data_ptr, *s_is_contiguous, *s_nbytes, *s_cuda_stream;
+static PyObject *s_data_ptr, *s_is_contiguous, *s_nbytes, *s_cuda_stream, *s_dtype;
 static PyObject *f_raw_stream, *f_device;      /* current stream of a device, current device */
 
 /* address of a tensor; None = NULL, an integer is an address */
@@ -234,9 +234,27 @@ static PyObject *init(PyObject *self, PyObject *args)
     Py_RETURN_NONE;
 }
 
+/* fit(mapping, tensor, mapping, tensor, ...): mapping[tensor.dtype] has to be there, or its __missing__ says what is wrong; an address and None have no dtype */
+static PyObject *fit(PyObject *self, PyObject *const *o, Py_ssize_t count)
+{
+    (void)self;
+    for (Py_ssize_t i = 0; i + 1 < count; i += 2) {
+        if (o[i + 1] == Py_None || PyLong_Check(o[i + 1])) continue;
+        PyObject *dtype = PyObject_GetAttr(o[i + 1], s_dtype);
+        if (!dtype) return NULL;
+        const int known = PyDict_Contains(o[i], dtype);
+        PyObject *found = known == 0 ? PyObject_GetItem(o[i], dtype) : NULL;
+        Py_DECREF(dtype);
+        Py_XDECREF(found);
+        if (known < 0 || (known == 0 && !found)) return NULL;
+    }
+    Py_RETURN_NONE;
+}
+
 static PyMethodDef methods[] = {
 #define METHOD(NAME, FORMAT, ARGS) {#NAME, (PyCFunction)(void (*)(void))py_##NAME, METH_FASTCALL, FORMAT},
-    CALLS(METHOD){"init", init, METH_VARARGS, "function addresses of libcdl by name, and torch's stream and device queries"},
+    CALLS(METHOD){"fit", (PyCFunction)(void (*)(void))fit, METH_FASTCALL, "dtypes of tensors against those that fit"},
+    {"init", init, METH_VARARGS, "function addresses of libcdl by name, and torch's stream and device queries"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "libcdl calls", -1, methods, NULL, NULL, NULL, NULL};
@@ -247,5 +265,6 @@ PyMODINIT_FUNC PyInit__marshal(void)
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_nbytes = PyUnicode_InternFromString("nbytes");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+    s_dtype = PyUnicode_InternFromString("dtype");
     return PyModule_Create(&module);
 }

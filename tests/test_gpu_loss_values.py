@@ -1,4 +1,4 @@
-"""The loss of the last layer where logits are infinite, the lowest or no numbers, and where weights are the largest."""
+"""The loss of the last layer where logits are infinite, the lowest or no numbers, and where weights are the largest; its gradients against differences that they cannot miss."""
 import pytest
 
 import gpu_util as gu
@@ -127,3 +127,47 @@ def test_fp32_weights_up_to_the_largest(env):
     assert ((got_lse.double() - lse).abs() <= error).all() and ((got_loss.double() - loss).abs() <= error).all()
     got_w = case.backward(got_lse, want_h=False)[1]
     assert float((got_w.double() - d_w)[:, 1:].norm()) <= 2e-5 * float(d_w[:, 1:].norm())
+
+
+def test_gradient_of_a_token_is_the_difference_of_its_loss(env):
+    """Every token for itself, along its own gradient, where the difference is largest."""
+    torch, _ = env
+    T, V, D, step = 40, 90, 64, 2.0 ** -5
+    case = Case(env, T, V, D, "float32", padding=0.0)
+    case.d_loss = torch.ones(T, device="cuda")
+    every, ok = torch.arange(V, device="cuda"), torch.ones(T, dtype=torch.bool, device="cuda")
+    case.d_lse = torch.zeros(T, device="cuda")
+    _, lse, way, _, error = formulas(torch, case, every, ok)
+    d_h, _ = case.backward(case.forward()[1])
+    way = (way / way.norm(dim=1, keepdim=True)).float()
+    high, low = (case.forward((case.h + sign * step * way).contiguous())[0].double() for sign in (1.0, -1.0))
+    moved = ((case.h + step * way).double() - (case.h - step * way).double()) / (2 * step)      # (what the rounding of h has left of the direction)
+    diff, along = (high - low) / (2 * step), (d_h.double() * moved).sum(dim=1)
+    # the third derivative is a third cumulant: at most the cube of the range of dz; either loss within its rounding (twice, for the moved h)
+    dz = moved @ case.w.double().t()
+    bound = (dz.amax(dim=1) - dz.amin(dim=1)) ** 3 * step ** 2 / 6 + 2 * error / step + 1e-5
+    assert (along > 10 * bound).all(), float((along / bound).min())      # zeros would not pass
+    assert ((diff - along).abs() <= bound).all()
+
+
+def test_gradient_of_the_vocabulary_is_the_difference_of_the_loss(env):
+    torch, _ = env
+    T, V, D, step = 40, 90, 64, 2.0 ** -4
+    case = Case(env, T, V, D, "float32", padding=0.1)
+    ok = (case.target >= 0) & (case.target < V)
+    case.d_lse = torch.zeros(T, device="cuda")
+    _, _, _, way, error = formulas(torch, case, torch.arange(V, device="cuda"), ok)
+    _, d_w = case.backward(case.forward()[1])
+    way = (way / way.norm()).float()
+    base, sums, moved = case.w, [], []
+    for sign in (1.0, -1.0):
+        case.w = base + sign * step * way
+        moved.append(case.w.double())
+        sums.append(case.forward()[0].double())
+    moved = (moved[0] - moved[1]) / (2 * step)
+    weight = case.d_loss.double() * ok
+    diff, along = float((weight * (sums[0] - sums[1])).sum()) / (2 * step), float((d_w.double() * moved).sum())
+    dz = case.h.double() @ moved.t()
+    bound = float((weight * ((dz.amax(dim=1) - dz.amin(dim=1)) ** 3 * step ** 2 / 6 + 2 * error / step)).sum()) + 1e-5
+    assert along > 10 * bound, along / bound
+    assert abs(diff - along) <= bound

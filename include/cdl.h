@@ -419,9 +419,9 @@ int cdl_block8_quantize(const void *x, int32_t type, int32_t rows, int32_t cols,
  *   y[m,n] = sum_kb a_scale[kb,m] * b_scale[kb,n] * sum_{k in block kb} a[m,k] * b[n,k]     (y[M,N], fp32 or bf16 by y_type)
  * a [M][pitch(K)] with a_scale [blocks of K][pitch(M)], b [N][pitch(K)] with b_scale [blocks of K][pitch(N)], as
  * cdl_block8_quantize writes them (bytes beyond K have to be zero; scale bytes 1 .. 254).  Into fp32: products are exact and sums
- * fp32 (an entry below 2^-126 in value counts as 0; the quantizer makes none).  Into bf16: the matrix instructions for
+ * fp32 (an entry below 2^-126 in value counts as 0, the quantizer makes none; one from 2^128 on as infinite, to which entries beyond 1.875 * 2^127 may round).  Into bf16: the matrix instructions for
  * 8-bit operands, at twice the rate, which of every product keep what lies above 2^-14 of the largest of the 16 that they
- * add up first (1.5e-5 of the result over random operands), sums in fp32, one rounding.  With x -> (q, scale) of the
+ * add up first (1.5e-5 of a typical result over random operands; more of one that cancels), sums in fp32, one rounding.  With x -> (q, scale) of the
  * activations, w -> tiles of the weights and g -> the gradient of the output,
  *   forward y = x . w^T          a = x,     b = w
  *   d_x = g . w                  a = g,     b = w's (q_t, scale_t)
@@ -448,7 +448,7 @@ int cdl_block8_gemm(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, 
  *   g[t,v] = (d_loss[t] + d_lse[t]) * exp(z[t,v] - lse[t]) - d_loss[t] * [v = target[t]],      d_loss[t] taken as 0 for padding,
  *   d_h[t,:] = sum_v g[t,v] w[v,:]   (type, [T,D], nullable),    d_w[v,:] = sum_t g[t,v] h[t,:]   (type, [V,D], nullable)
  * z is formed again, a piece of the vocabulary at a time; for bf16, g (divided by the largest |d_loss| + |d_lse|) is rounded to bf16
- * before its two products, all sums are fp32.  For fp32 every operand is used as three bf16 parts, which hold it whole, and the six
+ * before its two products (2^-9 of an entry at most: next to the rounding of the results, errors up to 1.4 times as large), all sums are fp32.  For fp32 every operand is used as three bf16 parts, which hold it whole, and the six
  * products of parts that matter in fp32 are summed.  At least one output.  Same inputs, same bits.
  * `train` != 0: scratch for the backward call too (the forward call takes either).  256-byte aligned, as for all calls.
  * V >= 1 unless T == 0 (CDL_ERR_PARAM).  D == 0: z = 0.  CDL_ERR_RANGE for D > 2^20, T > 2^22, V > 2^30 or T * V > 2^44.

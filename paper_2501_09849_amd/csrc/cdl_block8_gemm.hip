@@ -2,8 +2,8 @@
 //
 //   y[m,n] = sum_kb 2^(a_scale[kb,m] + b_scale[kb,n] - 254) * sum_{k in kb} a[m,k] * b[n,k]
 //
-// Scales are powers of two, so the matrix instructions apply them.  65536 x 3072 x 768 into bf16 188 us, call after call, at the power limit, 221: 146 of them products and loads, 35
-// turning results into rows and 42 storing 403 MB, during both of which a compute unit's only block of 256 x 256 multiplies nothing; 3072 x 768 x 65536 into fp32 268 us, the matrix cores busy 62 %.
+// Scales are powers of two, so the matrix instructions apply them.  65536 x 3072 x 768 into bf16 185 us, call after call, at the power limit, 221: 146 of them products and loads, 35
+// turning results into rows and 42 storing 403 MB, during both of which a compute unit's only block of 256 x 256 multiplies nothing; 3072 x 768 x 65536 into fp32 256 us, the matrix cores busy 62 %.
 #include "cdl_ring.h"
 
 namespace cdl {

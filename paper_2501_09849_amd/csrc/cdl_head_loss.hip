@@ -20,7 +20,7 @@ using Square = RingForm<2, 2, 2, 2, 3, 2, 2>;      // 128 x 128
 using Thin = RingForm<4, 1, 1, 2, 3, 3, 2>;        // 128 x 64
 
 // The logit of a token's target, where it lies in the wave's part of a tile (entry `at` of its 32 TP): the one that the sums are made of, so that a sure
-// token's loss and gradient vanish.  Few parts hold any: the search is skipped there.  Every lane stores f(logit), those without a target to `spare`: no
+// token's loss and gradient vanish but for a rounding of the log-sum.  Few parts hold any: the search is skipped there.  Every lane stores f(logit), those without a target to `spare`: no
 // branch that lanes take apart, around which the compiler would have to move registers that hold addresses.
 template <class FORM, class F>
 __device__ __forceinline__ void find_target(const v16f (&acc)[FORM::TP][FORM::TQ], int j, int64_t at, int half, float *to, float *spare, const F &f)
@@ -233,7 +233,8 @@ void head_tokens_kernel(const int64_t *__restrict__ target, const float *__restr
     out[t] = k;
 }
 
-// g of a piece of the vocabulary, [T][ld], zeros from `cols` up to ld; PARTS: in three parts `plane` entries apart
+// g of a piece of the vocabulary, as bf16, the products' type (in 32 bits, gradients would be 1.66e-3 off instead of 1.7e-3 to 2.4e-3, by how tokens weigh and how likely targets are, and
+// two bf16 parts would double the products), [T][ld], zeros from `cols` up to ld; PARTS: in three parts `plane` entries apart
 template <class FORM, bool PARTS>
 struct Gradient {
     static constexpr int kStores = row_stores<FORM, bf16_t>();

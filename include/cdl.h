@@ -448,8 +448,10 @@ int cdl_block8_gemm(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, 
  *   g[t,v] = (d_loss[t] + d_lse[t]) * exp(z[t,v] - lse[t]) - d_loss[t] * [v = target[t]],      d_loss[t] taken as 0 for padding,
  *   d_h[t,:] = sum_v g[t,v] w[v,:]   (type, [T,D], nullable),    d_w[v,:] = sum_t g[t,v] h[t,:]   (type, [V,D], nullable)
  * z is formed again, a piece of the vocabulary at a time; for bf16, g (divided by the largest |d_loss| + |d_lse|) is rounded to bf16
- * before its two products (2^-9 of an entry at most: next to the rounding of the results, errors up to 1.4 times as large), all sums are fp32.  For fp32 every operand is used as three bf16 parts, which hold it whole, and the six
- * products of parts that matter in fp32 are summed.  At least one output.  Same inputs, same bits.
+ * before its two products (2^-8 of an entry at most, all of one below 2^-126: next to the rounding of the results, errors up to
+ * 1.4 times as large), all sums are fp32.  For fp32 every operand is used as three bf16 parts, which hold it whole, and the six
+ * products of parts that matter in fp32 are summed.  The matrix cores take bf16 numbers below 2^-126 as 0: smaller entries of h and w (fp32: the last parts of entries
+ * below 2^-110) do not count.  At least one output.  Same inputs, same bits.
  * `train` != 0: scratch for the backward call too (the forward call takes either).  256-byte aligned, as for all calls.
  * V >= 1 unless T == 0 (CDL_ERR_PARAM).  D == 0: z = 0.  CDL_ERR_RANGE for D > 2^20, T > 2^22, V > 2^30 or T * V > 2^44.
  */

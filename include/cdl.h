@@ -14,7 +14,8 @@
  * third), cdl_qconv_fwd / cdl_qconv_bwd_weights / cdl_qconv_bwd_activations (a convolutional layer on [B,H,W,C]
  * activations), cdl_quantize_fwd_static (no workspace); next to the path: cdl_marginal_entropy, cdl_entropy_bwd,
  * cdl_quantize_draw, cdl_huffman_bits; layers in 8-bit floating point, their loss and dropout: cdl_block8_quantize, cdl_block8_gemm,
- * cdl_head_loss_fwd / cdl_head_loss_bwd, cdl_dropout.
+ * cdl_head_loss_fwd / cdl_head_loss_bwd, cdl_dropout; the feed-forward sublayer of such a network: cdl_layer_norm_fwd / cdl_layer_norm_bwd,
+ * cdl_block8_gemm_act, cdl_block8_gemm_gated, cdl_act_bwd, cdl_gated_bwd.
  *
  * Conventions for every entry point
  *   - All tensor and scalar-output pointers are DEVICE pointers owned by the caller; tensors are
@@ -472,6 +473,82 @@ int cdl_head_loss_bwd(const void *h, const void *w, int32_t type, const int64_t 
  */
 int cdl_dropout(const void *x, const void *add, int32_t type, int64_t n, float p, uint64_t seed, uint64_t counter,
                 void *y, void *hip_stream);
+
+/*
+ * ---- The feed-forward sublayer of a network in eight bits ------------------------------------------------------------
+ *
+ * Tensors are of `type` (CDL_F32, CDL_BF16), 16-byte aligned, as are the fp32 vectors of weights and biases; all sums, means and activations are formed in fp32
+ * and each output is rounded once.  Same inputs, same bits.  Outputs share no memory with inputs or with each other, unless it says so.  An entry that is not
+ * finite makes what its row (layer norm), its entry (activations) or its column (sums over the rows) holds not finite, and nothing else.
+ *
+ * Activations kept in eight bits.  Where a backward pass takes (q, scale, format) in the place of a tensor of `type`, these are its rows as cdl_block8_quantize writes
+ * them without tiles - q [rows][pitch(cols)], scale [blocks of cols][pitch(rows)], bytes 1 .. 254, or 255 for a block that is not finite -, half of the memory of bf16,
+ * and the pass is that of the values they stand for.  Either the tensor is given or both of q and scale, else CDL_ERR_NULL.
+ */
+
+/*
+ * Layer norm of the rows of x[rows, cols]:  y = (x - mean) rstd * weight + bias,  rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
+ *   weight, bias  fp32[cols], nullable (1 and 0);   y [rows, cols];   mean, rstd  fp32[rows], nullable
+ *   q, scale      nullable: x in eight bits for the backward pass, in the same pass over x and byte for byte what cdl_block8_quantize gives
+ * y may be x.  cols >= 1 unless rows == 0, eps finite and not negative (CDL_ERR_PARAM); CDL_ERR_RANGE for cols > 32768, rows > 2^30 or rows * cols > 2^44.
+ */
+int cdl_layer_norm_fwd(const void *x, int32_t type, const float *weight, const float *bias, int32_t rows, int32_t cols, float eps,
+                       void *y, float *mean, float *rstd, uint8_t *q, uint8_t *scale, int32_t format, void *hip_stream);
+/*
+ * Its gradients, with the mean and rstd of the forward call, from x or from its copy in eight bits:  n = (x - mean) rstd, h = g * weight,
+ *   d_x = rstd (h - mean of h - n * mean of (h n)) + add       ([rows, cols], nullable; add nullable (0): the gradient along a residual, say)
+ *   d_weight = sum over rows of g n,   d_bias = sum over rows of g      (fp32[cols], nullable; zeros for rows == 0)
+ * d_x may be g or add.  At least one output.  Limits as above.  Scratch: cdl_layer_norm_bwd_workspace_bytes, for d_weight and d_bias only.
+ */
+size_t cdl_layer_norm_bwd_workspace_bytes(int32_t rows, int32_t cols);
+int cdl_layer_norm_bwd(const void *g, int32_t type, const void *x, const uint8_t *q, const uint8_t *scale, int32_t format,
+                       const float *weight, const float *mean, const float *rstd, const void *add, int32_t rows, int32_t cols,
+                       void *d_x, float *d_weight, float *d_bias, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Activations: z, max(z, 0), z Phi(z) with the normal distribution's Phi, z / (1 + exp(-z)); their derivative at 0 of max(z, 0) is 0. */
+enum { CDL_ACT_NONE = 0, CDL_ACT_RELU = 1, CDL_ACT_GELU = 2, CDL_ACT_SILU = 3 };
+
+/*
+ * cdl_block8_gemm with what stands behind it in a layer:
+ *   z[m,n] = (the product of cdl_block8_gemm)[m,n] + bias[n],       y[m,n] = act(z[m,n]) + add[m,n]
+ *   bias  fp32[N], nullable;   add  [M,N], nullable (a residual);   y [M,N] required;   z [M,N] nullable, for the backward pass
+ * y, add and z are of y_type, which decides on the product's instructions as it does there; z is formed in fp32 and rounded where it is stored, y is of the
+ * unrounded one.  y may be add.  K == 0: the product is 0.  Errors and limits as for cdl_block8_gemm, and CDL_ERR_PARAM for an unknown activation.
+ * Scratch: cdl_block8_gemm_act_workspace_bytes.
+ */
+size_t cdl_block8_gemm_act_workspace_bytes(int32_t M, int32_t N, int32_t K);
+int cdl_block8_gemm_act(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale,
+                        int32_t M, int32_t N, int32_t K, int32_t a_format, int32_t b_format, const float *bias, int32_t act,
+                        const void *add, void *y, void *z, int32_t y_type, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * The gated product of two projections of a, each a matrix [N][pitch(K)] with scales of its own, both of b_format:
+ *   z_gate = a . b_gate^T + bias_gate,   z_up = a . b_up^T + bias_up,       y = act(z_gate) * z_up
+ * z_gate, z_up [M,N]: nullable, each by itself.  All else as for cdl_block8_gemm_act.
+ */
+size_t cdl_block8_gemm_gated_workspace_bytes(int32_t M, int32_t N, int32_t K);
+int cdl_block8_gemm_gated(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b_gate, const uint8_t *b_gate_scale,
+                          const uint8_t *b_up, const uint8_t *b_up_scale, int32_t M, int32_t N, int32_t K, int32_t a_format, int32_t b_format,
+                          const float *bias_gate, const float *bias_up, int32_t act, void *y, void *z_gate, void *z_up, int32_t y_type,
+                          void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Backward passes of what stands behind the products, for the gradient g[rows, cols] of y, from z or from its rows in eight bits:
+ *   d_z = g * act'(z),   d_bias = sum over rows of d_z
+ *   d_gate = g * z_up * act'(z_gate),   d_up = g * act(z_gate),   d_bias_gate, d_bias_up = their sums over rows
+ *   y = act(z), act(z_gate) * z_up: formed again, for a caller who has not kept it (of act, without the residual)
+ * All outputs are nullable, one of them has to be there; gradients and y are [rows, cols] of `type`, biases fp32[cols] (of the unrounded gradients; zeros for
+ * rows == 0).  The gradient of a product's residual is g itself; the products' gradients are cdl_block8_gemm's, of d_z in eight bits.  Any output of `type` may be g, z, z_gate
+ * or z_up (two outputs not the same).  The gated call takes both z or both in eight bits.  CDL_ERR_RANGE for cols > 2^24, rows > 2^30 or rows * cols > 2^44.
+ * Scratch: cdl_act_bwd_workspace_bytes, cdl_gated_bwd_workspace_bytes, for the biases only.
+ */
+size_t cdl_act_bwd_workspace_bytes(int32_t rows, int32_t cols);
+int cdl_act_bwd(const void *g, int32_t type, const void *z, const uint8_t *q, const uint8_t *scale, int32_t format, int32_t act, int32_t rows, int32_t cols,
+                void *d_z, float *d_bias, void *y, void *ws, size_t ws_bytes, void *hip_stream);
+size_t cdl_gated_bwd_workspace_bytes(int32_t rows, int32_t cols);
+int cdl_gated_bwd(const void *g, int32_t type, const void *z_gate, const void *z_up, const uint8_t *q_gate, const uint8_t *scale_gate,
+                  const uint8_t *q_up, const uint8_t *scale_up, int32_t format, int32_t act, int32_t rows, int32_t cols,
+                  void *d_gate, void *d_up, float *d_bias_gate, float *d_bias_up, void *y, void *ws, size_t ws_bytes, void *hip_stream);
 
 /*
  * Optional per-kernel timing (a measurement aid, not part of the method).  While enabled, every

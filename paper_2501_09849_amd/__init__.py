@@ -13,5 +13,8 @@ from .binding import (  # noqa: F401
     cdl_quantize_draw, cdl_entropy_bwd, huffman_workspace_bytes, cdl_huffman_bits,
     F32, BF16, E4M3, E5M2, block8_pitch, cdl_block8_quantize, block8_gemm_workspace_bytes, cdl_block8_gemm,
     head_loss_workspace_bytes, cdl_head_loss_fwd, cdl_head_loss_bwd, cdl_dropout,
+    ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU, cdl_layer_norm_fwd, layer_norm_bwd_workspace_bytes, cdl_layer_norm_bwd,
+    block8_gemm_act_workspace_bytes, cdl_block8_gemm_act, block8_gemm_gated_workspace_bytes, cdl_block8_gemm_gated,
+    act_bwd_workspace_bytes, cdl_act_bwd, gated_bwd_workspace_bytes, cdl_gated_bwd,
     cdl_profile_enable, cdl_profile_collect, cdl_profile_only, cdl_probe_mfma_int8, EXPORTS,
 )

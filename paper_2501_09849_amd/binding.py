@@ -19,7 +19,8 @@ _CALLS = None      # the native module, once the library is loaded
 _MARSHALLED = ("cdl_quantize_fwd", "cdl_quantize_bwd", "cdl_marginal_entropy", "cdl_quantize_draw", "cdl_entropy_bwd", "cdl_huffman_bits",
                "cdl_qgemm_fwd_offset", "cdl_qgemm_bwd_offset", "cdl_qgemm_fwd_quantize", "cdl_qconv_fwd", "cdl_qconv_bwd_weights",
                "cdl_qconv_bwd_activations", "cdl_qgemm_bwd_quantize_bwd", "cdl_block8_quantize", "cdl_block8_gemm", "cdl_head_loss_fwd",
-               "cdl_head_loss_bwd", "cdl_dropout")
+               "cdl_head_loss_bwd", "cdl_dropout", "cdl_layer_norm_fwd", "cdl_layer_norm_bwd", "cdl_block8_gemm_act", "cdl_block8_gemm_gated",
+               "cdl_act_bwd", "cdl_gated_bwd")
 
 EXPORTS = (
     "cdl_quantize_workspace_bytes", "cdl_qgemm_fwd_workspace_bytes", "cdl_qgemm_bwd_workspace_bytes",
@@ -31,12 +32,15 @@ EXPORTS = (
     "cdl_quantize_draw", "cdl_entropy_bwd", "cdl_huffman_workspace_bytes", "cdl_huffman_bits",
     "cdl_block8_pitch", "cdl_block8_quantize", "cdl_block8_gemm_workspace_bytes", "cdl_block8_gemm",
     "cdl_head_loss_workspace_bytes", "cdl_head_loss_fwd", "cdl_head_loss_bwd", "cdl_dropout",
+    "cdl_layer_norm_fwd", "cdl_layer_norm_bwd_workspace_bytes", "cdl_layer_norm_bwd", "cdl_block8_gemm_act_workspace_bytes", "cdl_block8_gemm_act",
+    "cdl_block8_gemm_gated_workspace_bytes", "cdl_block8_gemm_gated", "cdl_act_bwd_workspace_bytes", "cdl_act_bwd", "cdl_gated_bwd_workspace_bytes", "cdl_gated_bwd",
     "cdl_profile_enable", "cdl_profile_collect", "cdl_profile_only", "cdl_probe_mfma_int8",
     "cdl_status_string", "cdl_last_hip_error", "cdl_version",
 )
 
 F32, BF16 = 0, 1          # element types
 E4M3, E5M2 = 0, 1         # formats of 8-bit floating point
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 
 
 class CdlError(RuntimeError):
@@ -166,6 +170,24 @@ def load():
         L.cdl_head_loss_bwd.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, sz, vp]
         L.cdl_dropout.restype = ctypes.c_int
         L.cdl_dropout.argtypes = [vp, vp, i32, i64, f32, u64, u64, vp, vp]
+        for name in ("layer_norm_bwd", "act_bwd", "gated_bwd"):
+            query = getattr(L, "cdl_%s_workspace_bytes" % name)
+            query.restype, query.argtypes = sz, [i32, i32]
+        for name in ("block8_gemm_act", "block8_gemm_gated"):
+            query = getattr(L, "cdl_%s_workspace_bytes" % name)
+            query.restype, query.argtypes = sz, [i32, i32, i32]
+        L.cdl_layer_norm_fwd.restype = ctypes.c_int
+        L.cdl_layer_norm_fwd.argtypes = [vp, i32, vp, vp, i32, i32, f32, vp, vp, vp, vp, vp, i32, vp]
+        L.cdl_layer_norm_bwd.restype = ctypes.c_int
+        L.cdl_layer_norm_bwd.argtypes = [vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.cdl_block8_gemm_act.restype = ctypes.c_int
+        L.cdl_block8_gemm_act.argtypes = [vp] * 4 + [i32] * 5 + [vp, i32, vp, vp, vp, i32, vp, sz, vp]
+        L.cdl_block8_gemm_gated.restype = ctypes.c_int
+        L.cdl_block8_gemm_gated.argtypes = [vp] * 6 + [i32] * 5 + [vp, vp, i32, vp, vp, vp, i32, vp, sz, vp]
+        L.cdl_act_bwd.restype = ctypes.c_int
+        L.cdl_act_bwd.argtypes = [vp, i32, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.cdl_gated_bwd.restype = ctypes.c_int
+        L.cdl_gated_bwd.argtypes = [vp, i32] + [vp] * 6 + [i32] * 4 + [vp] * 6 + [sz, vp]
         L.cdl_profile_enable.restype = ctypes.c_int
         L.cdl_profile_enable.argtypes = [ctypes.c_int]
         L.cdl_profile_only.restype = ctypes.c_int
@@ -430,6 +452,74 @@ def cdl_dropout(x, n, p, seed, counter, y, add=None, stream=None, type=None):
     like = _TYPES.get(kind, _FLOATS)
     calls.fit(like, add, like, y)
     _check(calls.cdl_dropout(x, add, kind, n, p, seed, counter, y, stream), "cdl_dropout")
+
+
+def cdl_layer_norm_fwd(x, rows, cols, y, mean=None, rstd=None, weight=None, bias=None, eps=1e-5, q=None, scale=None, format=E4M3, stream=None, type=None):
+    calls, kind = _CALLS or _calls(), _type_of(x, type)
+    calls.fit(_TYPES.get(kind, _FLOATS), y, _FLOATS, weight, _FLOATS, bias, _FLOATS, mean, _FLOATS, rstd, _VALUES.get(format, _SCALES), q, _SCALES, scale)
+    _check(calls.cdl_layer_norm_fwd(x, kind, weight, bias, rows, cols, eps, y, mean, rstd, q, scale, format, stream), "cdl_layer_norm_fwd")
+
+
+def layer_norm_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load().cdl_layer_norm_bwd_workspace_bytes(rows, cols))
+
+
+def cdl_layer_norm_bwd(g, rows, cols, mean, rstd, d_x=None, d_weight=None, d_bias=None, x=None, q=None, scale=None, weight=None, add=None, ws=None, format=E4M3,
+                       stream=None, type=None):
+    calls, kind = _CALLS or _calls(), _type_of(g, type)
+    like = _TYPES.get(kind, _FLOATS)
+    calls.fit(like, x, like, add, like, d_x, _FLOATS, weight, _FLOATS, mean, _FLOATS, rstd, _FLOATS, d_weight, _FLOATS, d_bias, _VALUES.get(format, _SCALES), q, _SCALES, scale)
+    _check(calls.cdl_layer_norm_bwd(g, kind, x, q, scale, format, weight, mean, rstd, add, rows, cols, d_x, d_weight, d_bias, ws, stream), "cdl_layer_norm_bwd")
+
+
+def block8_gemm_act_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load().cdl_block8_gemm_act_workspace_bytes(M, N, K))
+
+
+def cdl_block8_gemm_act(a, a_scale, b, b_scale, M, N, K, y, z=None, bias=None, act=ACT_NONE, add=None, ws=None, stream=None, a_format=E4M3, b_format=E4M3, y_type=None):
+    calls, kind = _CALLS or _calls(), _type_of(y, y_type)
+    like = _TYPES.get(kind, _FLOATS)
+    calls.fit(_VALUES.get(a_format, _SCALES), a, _VALUES.get(b_format, _SCALES), b, _SCALES, a_scale, _SCALES, b_scale, _FLOATS, bias, like, add, like, z)
+    _check(calls.cdl_block8_gemm_act(a, a_scale, b, b_scale, M, N, K, a_format, b_format, bias, act, add, y, z, kind, ws, stream), "cdl_block8_gemm_act")
+
+
+def block8_gemm_gated_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load().cdl_block8_gemm_gated_workspace_bytes(M, N, K))
+
+
+def cdl_block8_gemm_gated(a, a_scale, b_gate, b_gate_scale, b_up, b_up_scale, M, N, K, y, z_gate=None, z_up=None, bias_gate=None, bias_up=None, act=ACT_SILU, ws=None,
+                          stream=None, a_format=E4M3, b_format=E4M3, y_type=None):
+    calls, kind = _CALLS or _calls(), _type_of(y, y_type)
+    like, values = _TYPES.get(kind, _FLOATS), _VALUES.get(b_format, _SCALES)
+    calls.fit(_VALUES.get(a_format, _SCALES), a, values, b_gate, values, b_up, _SCALES, a_scale, _SCALES, b_gate_scale, _SCALES, b_up_scale, _FLOATS, bias_gate,
+              _FLOATS, bias_up, like, z_gate, like, z_up)
+    _check(calls.cdl_block8_gemm_gated(a, a_scale, b_gate, b_gate_scale, b_up, b_up_scale, M, N, K, a_format, b_format, bias_gate, bias_up, act, y, z_gate, z_up, kind,
+                                       ws, stream), "cdl_block8_gemm_gated")
+
+
+def act_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load().cdl_act_bwd_workspace_bytes(rows, cols))
+
+
+def cdl_act_bwd(g, rows, cols, act, d_z=None, d_bias=None, y=None, z=None, q=None, scale=None, ws=None, format=E4M3, stream=None, type=None):
+    calls, kind = _CALLS or _calls(), _type_of(g, type)
+    like = _TYPES.get(kind, _FLOATS)
+    calls.fit(like, z, like, d_z, like, y, _FLOATS, d_bias, _VALUES.get(format, _SCALES), q, _SCALES, scale)
+    _check(calls.cdl_act_bwd(g, kind, z, q, scale, format, act, rows, cols, d_z, d_bias, y, ws, stream), "cdl_act_bwd")
+
+
+def gated_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load().cdl_gated_bwd_workspace_bytes(rows, cols))
+
+
+def cdl_gated_bwd(g, rows, cols, act, d_gate=None, d_up=None, d_bias_gate=None, d_bias_up=None, y=None, z_gate=None, z_up=None, q_gate=None, scale_gate=None, q_up=None,
+                  scale_up=None, ws=None, format=E4M3, stream=None, type=None):
+    calls, kind = _CALLS or _calls(), _type_of(g, type)
+    like, values = _TYPES.get(kind, _FLOATS), _VALUES.get(format, _SCALES)
+    calls.fit(like, z_gate, like, z_up, like, d_gate, like, d_up, like, y, _FLOATS, d_bias_gate, _FLOATS, d_bias_up, values, q_gate, values, q_up, _SCALES, scale_gate,
+              _SCALES, scale_up)
+    _check(calls.cdl_gated_bwd(g, kind, z_gate, z_up, q_gate, scale_gate, q_up, scale_up, format, act, rows, cols, d_gate, d_up, d_bias_gate, d_bias_up, y, ws, stream),
+           "cdl_gated_bwd")
 
 
 def cdl_probe_mfma_int8(iters: int, random_operands: bool, blocks: int, sink, stream=None) -> float:

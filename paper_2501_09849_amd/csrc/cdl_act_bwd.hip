@@ -1,0 +1,225 @@
+// Backward passes of what stands behind a product: the activation of a layer, and the gated product of two projections, from their values before it (z) as they are or
+// as kept in 8-bit floating point, with the sums over the rows that are the biases' gradients.
+//
+//   d_z = g act'(z),  y = act(z)          d_gate = g z_up act'(z_gate),  d_up = g act(z_gate),  y = act(z_gate) z_up
+#include "cdl_act.h"
+#include "cdl_block8.h"
+#include "cdl_chunks.h"
+
+namespace cdl {
+namespace {
+
+// A block: 256 columns, 32 lanes of eight each, eight rows at a time of its stretch of rows; a thread's sums of its columns stay in registers.
+constexpr int kLanes = 32, kGroups = 8, kThreads = kLanes * kGroups, kCols = kLanes * 8;
+
+struct ActBwd {
+    const void *g, *z[2];                 // z of the gate (or of the layer), and of the other projection
+    const uint8_t *q[2], *scale[2];
+    int rows, cols, col_blocks, rows_per;
+    void *d[2], *y;
+    float *parts;                         // [stretch of rows][1 or 2][part_cols], or null
+    int64_t pitch_c, pitch_r, part_cols;
+    bool stream;
+};
+
+template <class T, int ACT, bool GATED, bool RAGGED, int KEPT>      // KEPT: 0 no, 1 E4M3, 2 E5M2
+__global__ __launch_bounds__(kThreads)
+void act_bwd_kernel(ActBwd a)
+{
+    constexpr int S = GATED ? 2 : 1;
+    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+    const int cb = (int)(blockIdx.x % (unsigned)a.col_blocks), part = (int)(blockIdx.x / (unsigned)a.col_blocks);
+    const int col = cb * kCols + lane * 8, left = a.cols - col;
+    const int64_t first = (int64_t)part * a.rows_per, end = min(first + a.rows_per, (int64_t)a.rows);
+    Raw8<T> raw_g, raw_z[S];
+    u32x2 kept[S];
+    uint32_t byte[S];
+    auto fetch = [&](int64_t r) {
+        const int64_t at = r * a.cols + col;
+        raw_g = load_raw<RAGGED>((const T *)a.g + at, left, a.stream);
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            if (KEPT) {
+                if (left > 0) {
+                    kept[s] = *reinterpret_cast<const u32x2 *>(a.q[s] + r * a.pitch_c + col);
+                    byte[s] = a.scale[s][(int64_t)(col >> 7) * a.pitch_r + r];
+                } else {
+                    kept[s] = u32x2{0, 0};
+                    byte[s] = 127;
+                }
+            } else {
+                raw_z[s] = load_raw<RAGGED>((const T *)a.z[s] + at, left, a.stream);
+            }
+        }
+    };
+    float sums[S][8];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sums[s][k] = 0.0f;
+    int64_t row = first + group;
+    if (row < end) fetch(row);
+    for (; row < end; row += kGroups) {
+        float g[8], z[S][8], d[S][8], y[8];
+        unpack(raw_g, g);
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            if (KEPT) {
+                values8<KEPT == 2>(kept[s], z[s]);
+                const float by = scale_of(byte[s]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) z[s][k] *= by;
+            } else {
+                unpack(raw_z[s], z[s]);
+            }
+        }
+        if (row + kGroups < end) fetch(row + kGroups);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const ValueSlope v = act_both<ACT>(z[0][k]);
+            if constexpr (GATED) {
+                d[0][k] = g[k] * z[1][k] * v.slope;
+                d[1][k] = g[k] * v.value;
+                y[k] = v.value * z[1][k];
+            } else {
+                d[0][k] = g[k] * v.slope;
+                y[k] = v.value;
+            }
+#pragma unroll
+            for (int s = 0; s < S; ++s) sums[s][k] += d[s][k];
+        }
+        const int64_t at = row * a.cols + col;
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+            if (a.d[s]) store_first<RAGGED>((T *)a.d[s] + at, left, d[s], a.stream);
+        if (a.y) store_first<RAGGED>((T *)a.y + at, left, y, a.stream);
+    }
+    if (!a.parts) return;
+    __shared__ float all[kGroups][kCols];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        if (s > 0) __syncthreads();
+        store8(&all[group][lane * 8], sums[s], false);
+        __syncthreads();
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) sum += all[i][threadIdx.x];
+        if (cb * kCols + (int)threadIdx.x < a.cols) a.parts[((int64_t)part * S + s) * a.part_cols + cb * kCols + threadIdx.x] = sum;
+    }
+}
+
+// Sums of the blocks' parts [parts][sets][pitch] over the first index, in order: 16 columns a block, 64 threads each.
+__global__ __launch_bounds__(1024)
+void column_sums_kernel(const float *__restrict__ parts, int64_t n, int sets, int64_t cols, int64_t pitch, float *out0, float *out1)
+{
+    __shared__ float all[64][16];
+    const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+    const int64_t col = (int64_t)blockIdx.x * 16 + lane;
+    float *const out = blockIdx.y ? out1 : out0;
+    if (!out) return;
+    float sum = 0.0f;
+    if (col < cols) {
+#pragma unroll 8
+        for (int64_t i = group; i < n; i += 64) sum += parts[(i * sets + blockIdx.y) * pitch + col];
+    }
+    all[group][lane] = sum;
+    __syncthreads();
+    if (threadIdx.x < 16 && col < cols) {
+        sum = 0.0f;
+        for (int i = 0; i < 64; ++i) sum += all[i][lane];
+        out[col] = sum;
+    }
+}
+
+int64_t part_cols(int32_t cols) { return ((int64_t)cols + 7) / 8 * 8; }
+
+// Stretches of rows: blocks that fill the chip, of at least 16 rows.
+struct Split { int col_blocks, parts, rows_per; };
+Split split_of(int32_t rows, int32_t cols)
+{
+    Split s;
+    s.col_blocks = (cols + kCols - 1) / kCols;
+    int64_t parts = (2048 + s.col_blocks - 1) / s.col_blocks;
+    const int64_t most = ((int64_t)rows + 15) / 16;
+    if (parts > most) parts = most;
+    s.rows_per = (int)((rows + parts - 1) / parts);
+    s.parts = (rows + s.rows_per - 1) / s.rows_per;
+    return s;
+}
+
+template <class T, int ACT, bool GATED, bool RAGGED>
+int launch_act(const ActBwd &a, int kept, int64_t blocks, hipStream_t stream)
+{
+    const auto kernel = kept == 0 ? act_bwd_kernel<T, ACT, GATED, RAGGED, 0> : kept == 1 ? act_bwd_kernel<T, ACT, GATED, RAGGED, 1> : act_bwd_kernel<T, ACT, GATED, RAGGED, 2>;
+    CDL_LAUNCH(GATED ? "gated_bwd_kernel" : "act_bwd_kernel", stream, kernel, dim3((unsigned)blocks), dim3(kThreads), 0, a);
+    return check_launch();
+}
+template <class T, bool GATED, bool RAGGED>
+int launch_any(const ActBwd &a, int act, int kept, int64_t blocks, hipStream_t stream)
+{
+    switch (act) {
+        case CDL_ACT_RELU: return launch_act<T, CDL_ACT_RELU, GATED, RAGGED>(a, kept, blocks, stream);
+        case CDL_ACT_GELU: return launch_act<T, CDL_ACT_GELU, GATED, RAGGED>(a, kept, blocks, stream);
+        case CDL_ACT_SILU: return launch_act<T, CDL_ACT_SILU, GATED, RAGGED>(a, kept, blocks, stream);
+        default: return launch_act<T, CDL_ACT_NONE, GATED, RAGGED>(a, kept, blocks, stream);
+    }
+}
+template <bool GATED>
+int launch_all(ActBwd a, int type, int act, int kept, const Split &s, hipStream_t stream)
+{
+    const int64_t blocks = (int64_t)s.col_blocks * s.parts;
+    if (a.cols % 8 == 0)
+        return type == CDL_BF16 ? launch_any<bf16_t, GATED, false>(a, act, kept, blocks, stream) : launch_any<float, GATED, false>(a, act, kept, blocks, stream);
+    return type == CDL_BF16 ? launch_any<bf16_t, GATED, true>(a, act, kept, blocks, stream) : launch_any<float, GATED, true>(a, act, kept, blocks, stream);
+}
+
+}  // namespace
+
+int launch_column_sums(const float *parts, int64_t n, int32_t cols, int64_t pitch, float *out0, float *out1, hipStream_t stream, int sets)
+{
+    const dim3 grid((unsigned)((cols + 15) / 16), (unsigned)sets);
+    CDL_LAUNCH("column_sums_kernel", stream, column_sums_kernel, grid, dim3(1024), 0, parts, n, sets, (int64_t)cols, pitch, out0, out1);
+    return check_launch();
+}
+
+size_t act_bwd_workspace_bytes(int32_t rows, int32_t cols, bool gated)
+{
+    if (rows == 0 || cols == 0) return 0;
+    return align_up((size_t)split_of(rows, cols).parts * (gated ? 2 : 1) * (size_t)part_cols(cols) * sizeof(float), 256);
+}
+
+int launch_act_bwd(const ActCall &c, bool gated, hipStream_t stream)
+{
+    if (c.cols == 0) return CDL_OK;
+    const bool sums = c.d_bias[0] || c.d_bias[1];
+    const int64_t size = c.type == CDL_BF16 ? 2 : 4;
+    int64_t parts = 0;
+    if (c.rows > 0) {
+        const Split s = split_of(c.rows, c.cols);
+        parts = s.parts;
+        ActBwd a{};
+        a.g = c.g;
+        for (int i = 0; i < 2; ++i) {
+            a.z[i] = c.z[i];
+            a.q[i] = c.q[i];
+            a.scale[i] = c.scale[i];
+            a.d[i] = c.d[i];
+        }
+        a.rows = c.rows;
+        a.cols = c.cols;
+        a.col_blocks = s.col_blocks;
+        a.rows_per = s.rows_per;
+        a.y = c.y;
+        a.parts = sums ? (float *)c.ws : nullptr;
+        a.pitch_c = block8_pitch(c.cols);
+        a.pitch_r = block8_pitch(c.rows);
+        a.part_cols = part_cols(c.cols);
+        a.stream = (int64_t)c.rows * c.cols * size >= kStreamFrom * 4;
+        const int kept = !c.q[0] ? 0 : c.format == CDL_E5M2 ? 2 : 1;
+        const int rc = gated ? launch_all<true>(a, c.type, c.act, kept, s, stream) : launch_all<false>(a, c.type, c.act, kept, s, stream);
+        if (rc != CDL_OK) return rc;
+    }
+    return sums ? launch_column_sums((const float *)c.ws, parts, c.cols, part_cols(c.cols), c.d_bias[0], c.d_bias[1], stream, gated ? 2 : 1) : CDL_OK;
+}
+
+}  // namespace cdl

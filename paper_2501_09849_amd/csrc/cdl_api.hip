@@ -5,6 +5,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <random>
 #include <vector>
@@ -577,6 +578,138 @@ int cdl_dropout(const void *x, const void *add, int32_t type, int64_t n, float p
     if (n > 0 && (!x || !y)) return CDL_ERR_NULL;
     if (!aligned(x, 16) || !aligned(add, 16) || !aligned(y, 16)) return CDL_ERR_ALIGN;
     return launch_dropout(x, add, type, n, p, seed, counter, y, (hipStream_t)hip_stream);
+}
+
+// ---- a feed-forward sublayer ------------------------------------------------------------------
+
+namespace {
+bool act_ok(int32_t act) { return act == CDL_ACT_NONE || act == CDL_ACT_RELU || act == CDL_ACT_GELU || act == CDL_ACT_SILU; }
+bool all_aligned(std::initializer_list<const void *> pointers)
+{
+    for (const void *p : pointers)
+        if (!aligned(p, 16)) return false;
+    return true;
+}
+// a tensor, or its rows in eight bits
+bool one_of(const void *z, const uint8_t *q, const uint8_t *scale) { return z ? !q && !scale : q && scale; }
+bool norm_ok(int32_t rows, int32_t cols) { return cols <= kNormMostCols && rows <= 1 << 30 && (int64_t)rows * cols <= (int64_t)1 << 44; }
+bool rows_ok(int32_t rows, int32_t cols) { return cols <= 1 << 24 && rows <= 1 << 30 && (int64_t)rows * cols <= (int64_t)1 << 44; }
+bool product_ok(int32_t M, int32_t N, int32_t K) { return K <= 1 << 23 && M <= 1 << 30 && N <= 1 << 30 && (int64_t)M * N <= (int64_t)1 << 44; }
+}
+
+int cdl_layer_norm_fwd(const void *x, int32_t type, const float *weight, const float *bias, int32_t rows, int32_t cols, float eps,
+                       void *y, float *mean, float *rstd, uint8_t *q, uint8_t *scale, int32_t format, void *hip_stream)
+{
+    if (rows < 0 || cols < 0 || (rows > 0 && cols < 1) || !type_ok(type) || !format_ok(format) || !(std::isfinite(eps) && eps >= 0.0f)) return CDL_ERR_PARAM;
+    if (!norm_ok(rows, cols)) return CDL_ERR_RANGE;
+    if (!q != !scale || (rows > 0 && (!x || !y))) return CDL_ERR_NULL;
+    if (!all_aligned({x, weight, bias, y, q, scale}) || !aligned(mean, 4) || !aligned(rstd, 4)) return CDL_ERR_ALIGN;
+    return launch_layer_norm_fwd(x, type, weight, bias, rows, cols, eps, y, mean, rstd, q, scale, format, (hipStream_t)hip_stream);
+}
+
+size_t cdl_layer_norm_bwd_workspace_bytes(int32_t rows, int32_t cols)
+{
+    if (rows < 0 || cols < 1 || !norm_ok(rows, cols)) return 0;
+    return layer_norm_bwd_workspace_bytes(rows, cols);
+}
+
+int cdl_layer_norm_bwd(const void *g, int32_t type, const void *x, const uint8_t *q, const uint8_t *scale, int32_t format,
+                       const float *weight, const float *mean, const float *rstd, const void *add, int32_t rows, int32_t cols,
+                       void *d_x, float *d_weight, float *d_bias, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    if (rows < 0 || cols < 0 || (rows > 0 && cols < 1) || !type_ok(type) || !format_ok(format)) return CDL_ERR_PARAM;
+    if (!norm_ok(rows, cols)) return CDL_ERR_RANGE;
+    if ((!d_x && !d_weight && !d_bias) || (rows > 0 && (!g || !one_of(x, q, scale) || !mean || !rstd))) return CDL_ERR_NULL;
+    if (!all_aligned({g, x, q, scale, weight, add, d_x, d_weight, d_bias}) || !aligned(mean, 4) || !aligned(rstd, 4)) return CDL_ERR_ALIGN;
+    if (cols == 0) return CDL_OK;
+    const int rc = check_ws(ws, ws_bytes, d_weight || d_bias ? layer_norm_bwd_workspace_bytes(rows, cols) : 0);
+    if (rc != CDL_OK) return rc;
+    return launch_layer_norm_bwd(g, type, x, q, scale, format, weight, mean, rstd, add, rows, cols, d_x, d_weight, d_bias, ws, (hipStream_t)hip_stream);
+}
+
+namespace {
+int check_product(const ProductCall &c, bool gated, size_t ws_bytes, hipStream_t stream)
+{
+    if (c.M < 0 || c.N < 0 || c.K < 0 || !format_ok(c.a_format) || !format_ok(c.b_format) || !type_ok(c.y_type) || !act_ok(c.act)) return CDL_ERR_PARAM;
+    if (!product_ok(c.M, c.N, c.K)) return CDL_ERR_RANGE;
+    if (c.M == 0 || c.N == 0) return CDL_OK;
+    if (!c.y || (c.K > 0 && (!c.a || !c.a_scale || !c.b[0] || !c.b_scale[0] || (gated && (!c.b[1] || !c.b_scale[1]))))) return CDL_ERR_NULL;
+    if (!all_aligned({c.a, c.a_scale, c.b[0], c.b_scale[0], c.b[1], c.b_scale[1], c.bias[0], c.bias[1], c.add, c.y, c.z[0], c.z[1]})) return CDL_ERR_ALIGN;
+    const int rc = check_ws(c.ws, ws_bytes, block8_gemm_act_workspace_bytes(c.M, c.N, c.K, gated));
+    if (rc != CDL_OK) return rc;
+    return launch_block8_gemm_act(c, gated, stream);
+}
+}
+
+size_t cdl_block8_gemm_act_workspace_bytes(int32_t M, int32_t N, int32_t K)
+{
+    if (M < 0 || N < 0 || K < 0 || !product_ok(M, N, K)) return 0;
+    return block8_gemm_act_workspace_bytes(M, N, K, false);
+}
+
+int cdl_block8_gemm_act(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale,
+                        int32_t M, int32_t N, int32_t K, int32_t a_format, int32_t b_format, const float *bias, int32_t act,
+                        const void *add, void *y, void *z, int32_t y_type, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    return check_product({a, a_scale, {b, nullptr}, {b_scale, nullptr}, M, N, K, a_format, b_format, {bias, nullptr}, act, add, y, {z, nullptr}, y_type, ws}, false, ws_bytes,
+                         (hipStream_t)hip_stream);
+}
+
+size_t cdl_block8_gemm_gated_workspace_bytes(int32_t M, int32_t N, int32_t K)
+{
+    if (M < 0 || N < 0 || K < 0 || !product_ok(M, N, K)) return 0;
+    return block8_gemm_act_workspace_bytes(M, N, K, true);
+}
+
+int cdl_block8_gemm_gated(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b_gate, const uint8_t *b_gate_scale,
+                          const uint8_t *b_up, const uint8_t *b_up_scale, int32_t M, int32_t N, int32_t K, int32_t a_format, int32_t b_format,
+                          const float *bias_gate, const float *bias_up, int32_t act, void *y, void *z_gate, void *z_up, int32_t y_type,
+                          void *ws, size_t ws_bytes, void *hip_stream)
+{
+    return check_product({a, a_scale, {b_gate, b_up}, {b_gate_scale, b_up_scale}, M, N, K, a_format, b_format, {bias_gate, bias_up}, act, nullptr, y, {z_gate, z_up}, y_type, ws},
+                         true, ws_bytes, (hipStream_t)hip_stream);
+}
+
+namespace {
+int check_act(const ActCall &c, bool gated, size_t ws_bytes, hipStream_t stream)
+{
+    if (c.rows < 0 || c.cols < 0 || !type_ok(c.type) || !format_ok(c.format) || !act_ok(c.act)) return CDL_ERR_PARAM;
+    if (!rows_ok(c.rows, c.cols)) return CDL_ERR_RANGE;
+    if (!c.d[0] && !c.d[1] && !c.d_bias[0] && !c.d_bias[1] && !c.y) return CDL_ERR_NULL;
+    if (!all_aligned({c.g, c.z[0], c.z[1], c.q[0], c.q[1], c.scale[0], c.scale[1], c.d[0], c.d[1], c.d_bias[0], c.d_bias[1], c.y})) return CDL_ERR_ALIGN;
+    const bool some = c.rows > 0 && c.cols > 0;
+    if (some && (!c.g || !one_of(c.z[0], c.q[0], c.scale[0]) || (gated && (!one_of(c.z[1], c.q[1], c.scale[1]) || !c.z[0] != !c.z[1])))) return CDL_ERR_NULL;
+    const int rc = check_ws(c.ws, ws_bytes, c.d_bias[0] || c.d_bias[1] ? act_bwd_workspace_bytes(c.rows, c.cols, gated) : 0);
+    if (rc != CDL_OK) return rc;
+    return launch_act_bwd(c, gated, stream);
+}
+}
+
+size_t cdl_act_bwd_workspace_bytes(int32_t rows, int32_t cols)
+{
+    if (rows < 0 || cols < 0 || !rows_ok(rows, cols)) return 0;
+    return act_bwd_workspace_bytes(rows, cols, false);
+}
+
+int cdl_act_bwd(const void *g, int32_t type, const void *z, const uint8_t *q, const uint8_t *scale, int32_t format, int32_t act, int32_t rows, int32_t cols,
+                void *d_z, float *d_bias, void *y, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    return check_act({g, type, {z, nullptr}, {q, nullptr}, {scale, nullptr}, format, act, rows, cols, {d_z, nullptr}, y, {d_bias, nullptr}, ws}, false, ws_bytes,
+                     (hipStream_t)hip_stream);
+}
+
+size_t cdl_gated_bwd_workspace_bytes(int32_t rows, int32_t cols)
+{
+    if (rows < 0 || cols < 0 || !rows_ok(rows, cols)) return 0;
+    return act_bwd_workspace_bytes(rows, cols, true);
+}
+
+int cdl_gated_bwd(const void *g, int32_t type, const void *z_gate, const void *z_up, const uint8_t *q_gate, const uint8_t *scale_gate,
+                  const uint8_t *q_up, const uint8_t *scale_up, int32_t format, int32_t act, int32_t rows, int32_t cols,
+                  void *d_gate, void *d_up, float *d_bias_gate, float *d_bias_up, void *y, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    return check_act({g, type, {z_gate, z_up}, {q_gate, q_up}, {scale_gate, scale_up}, format, act, rows, cols, {d_gate, d_up}, y, {d_bias_gate, d_bias_up}, ws}, true, ws_bytes,
+                     (hipStream_t)hip_stream);
 }
 
 int cdl_probe_mfma_int8(int32_t iters, int32_t random_operands, int32_t blocks, void *sink, double *ops, void *hip_stream)

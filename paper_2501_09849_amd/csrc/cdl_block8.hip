@@ -1,5 +1,5 @@
 // A matrix in 8-bit floating point with a power of two as scale for every block of 128 entries, and its transpose, in one pass.
-#include "cdl_types.h"
+#include "cdl_block8.h"
 
 namespace cdl {
 namespace {
@@ -11,47 +11,6 @@ namespace {
 // goes through LDS as words of eight bytes, eight rows of a column, so that its rows leave as 128 whole bytes too.
 // Bound by memory: 65536 x 768 in bf16, both forms, 49 us, 4.1 TB/s where a copy reaches 5.1 (38.5 us where the memory-side cache holds all of it).
 constexpr int kTile = 128, kThreads = 256;
-
-__device__ __forceinline__ uint32_t row16_max(uint32_t x)      // over the 16 lanes that hold a row
-{
-#define CDL_ROR(N) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + N, 0xf, 0xf, false))
-    CDL_ROR(8); CDL_ROR(4); CDL_ROR(2); CDL_ROR(1);
-#undef CDL_ROR
-    return x;
-}
-
-// A block's largest magnitude (bits of the float) -> its scale's byte: the exponent rounded up where the fraction is beyond 1.75, the
-// largest of both formats, less the format's own exponent `top`.  At least 2^-100: no entry that is not zero then stands for a value below
-// 2^-116, and all are normal numbers of bf16 (the matrix cores take smaller ones as zero).
-constexpr int kLeast = 27;
-__device__ __forceinline__ uint32_t scale_byte(uint32_t largest, int top)
-{
-    if (largest >= 0x7f800000u) return 255u;
-    return (uint32_t)max((int)((largest + 0x1fffffu) >> 23) - top, kLeast);
-}
-__device__ __forceinline__ float inverse(uint32_t byte)      // 2^(127 - byte)
-{
-    return __uint_as_float(byte == 255u ? 0x7fc00000u : (254u - byte) << 23);
-}
-
-template <bool E5M2>
-__device__ __forceinline__ u32x2 eight(const float (&v)[8])
-{
-    u32x2 q = {0, 0};
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        int w = 0;
-        if (E5M2) {
-            w = __builtin_amdgcn_cvt_pk_bf8_f32(v[4 * h], v[4 * h + 1], w, false);
-            w = __builtin_amdgcn_cvt_pk_bf8_f32(v[4 * h + 2], v[4 * h + 3], w, true);
-        } else {
-            w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h], v[4 * h + 1], w, false);
-            w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2], v[4 * h + 3], w, true);
-        }
-        q[h] = (uint32_t)w;
-    }
-    return q;
-}
 
 struct QuantArgs {
     const void *x;

@@ -135,6 +135,26 @@ int launch_product(const RingJob &job, const Layout &l, int a_format, int b_form
     }
 }
 
+RingJob job_of(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale, int32_t M, int32_t N, int32_t K, const Layout &l)
+{
+    RingJob job{};
+    job.P = b;
+    job.Q = a;
+    job.ldp = job.ldq = block8_pitch(K);
+    job.rowsP = N;
+    job.rowsQ = M;
+    job.nk = (int)(block8_pitch(K) / kRingRow);
+    job.tiles_p = l.tiles_p;
+    job.tiles_q = l.tiles_q;
+    job.splits = l.splits;
+    job.k_per = l.k_per;
+    job.sp = b_scale;
+    job.sq = a_scale;
+    job.pitch_sp = block8_pitch(N);
+    job.pitch_sq = block8_pitch(M);
+    return job;
+}
+
 }  // namespace
 
 size_t block8_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K)
@@ -157,22 +177,7 @@ int launch_block8_gemm(const uint8_t *a, const uint8_t *a_scale, const uint8_t *
         });
     }
     const Layout l = layout(M, N, K);
-    const int64_t ld = block8_pitch(K);
-    RingJob job{};
-    job.P = b;
-    job.Q = a;
-    job.ldp = job.ldq = ld;
-    job.rowsP = N;
-    job.rowsQ = M;
-    job.nk = (int)(ld / kRingRow);
-    job.tiles_p = l.tiles_p;
-    job.tiles_q = l.tiles_q;
-    job.splits = l.splits;
-    job.k_per = l.k_per;
-    job.sp = b_scale;
-    job.sq = a_scale;
-    job.pitch_sp = block8_pitch(N);
-    job.pitch_sq = block8_pitch(M);
+    const RingJob job = job_of(a, a_scale, b, b_scale, M, N, K, l);
     if (l.splits == 1)
         return y_type == CDL_BF16 ? launch_product<false>(job, l, a_format, b_format, (bf16_t *)y, M, N, stream) : launch_product<true>(job, l, a_format, b_format, (float *)y, M, N, stream);
     const int rc = y_type == CDL_BF16 ? launch_product<false>(job, l, a_format, b_format, (float *)ws, M, N, stream)
@@ -182,6 +187,16 @@ int launch_block8_gemm(const uint8_t *a, const uint8_t *a_scale, const uint8_t *
     if (y_type == CDL_BF16) CDL_LAUNCH("block8_sum_kernel", stream, block8_sum_kernel<bf16_t>, dim3(blocks), dim3(256), 0, (const float *)ws, l.splits, n, (bf16_t *)y);
     else CDL_LAUNCH("block8_sum_kernel", stream, block8_sum_kernel<float>, dim3(blocks), dim3(256), 0, (const float *)ws, l.splits, n, (float *)y);
     return check_launch();
+}
+
+// The product as fp32 sums of the parts of the contraction, parts[split][M][N], for a kernel that adds them up.
+int block8_parts(int32_t M, int32_t N, int32_t K) { return M == 0 || N == 0 || K == 0 ? 0 : layout(M, N, K).splits; }
+int launch_block8_parts(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale, int32_t M, int32_t N, int32_t K, int32_t a_format,
+                        int32_t b_format, bool exact, float *parts, hipStream_t stream)
+{
+    const Layout l = layout(M, N, K);
+    const RingJob job = job_of(a, a_scale, b, b_scale, M, N, K, l);
+    return exact ? launch_product<true>(job, l, a_format, b_format, parts, M, N, stream) : launch_product<false>(job, l, a_format, b_format, parts, M, N, stream);
 }
 
 }  // namespace cdl

@@ -238,6 +238,46 @@ int launch_head_loss_bwd(const void *h, const void *w, int32_t type, const int64
                          int32_t T, int32_t V, int32_t D, void *d_h, void *d_w, void *ws, hipStream_t stream);
 int launch_dropout(const void *x, const void *add, int32_t type, int64_t n, float p, uint64_t seed, uint64_t counter, void *y, hipStream_t stream);      // (cdl_dropout.hip)
 
+int block8_parts(int32_t M, int32_t N, int32_t K);      // parts of the contraction, 0 where there is nothing to multiply
+int launch_block8_parts(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale, int32_t M, int32_t N, int32_t K, int32_t a_format,
+                        int32_t b_format, bool exact, float *parts, hipStream_t stream);
+
+// ---- a feed-forward sublayer ----------------------------------------------------------------
+constexpr int32_t kNormMostCols = 32768;
+int launch_layer_norm_fwd(const void *x, int32_t type, const float *weight, const float *bias, int32_t rows, int32_t cols, float eps, void *y, float *mean, float *rstd,
+                          uint8_t *q, uint8_t *scale, int32_t format, hipStream_t stream);      // (cdl_layer_norm.hip)
+size_t layer_norm_bwd_workspace_bytes(int32_t rows, int32_t cols);
+int launch_layer_norm_bwd(const void *g, int32_t type, const void *x, const uint8_t *q, const uint8_t *scale, int32_t format, const float *weight, const float *mean,
+                          const float *rstd, const void *add, int32_t rows, int32_t cols, void *d_x, float *d_weight, float *d_bias, void *ws, hipStream_t stream);
+// A product with what stands behind it, and the gated product of two (cdl_block8_act.hip): index 0 the layer or the gate, 1 the other projection.
+struct ProductCall {
+    const uint8_t *a, *a_scale, *b[2], *b_scale[2];
+    int32_t M, N, K, a_format, b_format;
+    const float *bias[2];
+    int32_t act;
+    const void *add;
+    void *y, *z[2];
+    int32_t y_type;
+    void *ws;
+};
+size_t block8_gemm_act_workspace_bytes(int32_t M, int32_t N, int32_t K, bool gated);
+int launch_block8_gemm_act(const ProductCall &call, bool gated, hipStream_t stream);
+// Their backward passes up to the products (cdl_act_bwd.hip).
+struct ActCall {
+    const void *g;
+    int32_t type;
+    const void *z[2];
+    const uint8_t *q[2], *scale[2];
+    int32_t format, act, rows, cols;
+    void *d[2], *y;
+    float *d_bias[2];
+    void *ws;
+};
+size_t act_bwd_workspace_bytes(int32_t rows, int32_t cols, bool gated);
+int launch_act_bwd(const ActCall &call, bool gated, hipStream_t stream);
+// Sums of parts[n][sets][pitch] over the first index into out0 and out1, one for each set (of which either may be null).
+int launch_column_sums(const float *parts, int64_t n, int32_t cols, int64_t pitch, float *out0, float *out1, hipStream_t stream, int sets = 2);
+
 int launch_mfma_probe(int iters, int random_operands, int blocks, int *sink, hipStream_t stream);
 
 }  // namespace cdl

@@ -1,0 +1,378 @@
+// Layer norm of the rows of a matrix, its gradients, and the rows' copy in 8-bit floating point from which the backward pass can be formed.
+//
+//   m = mean of the row, r = 1 / sqrt(mean of (x - m)^2 + eps), c = (x - m) r;     y = c w + b
+//   h = g w:   d_x = r (h - mean of h - c mean of (h c)) + add,     d_w = sum over rows of g c,     d_b = sum over rows of g
+//
+// A row stays in the registers of L lanes, C chunks of eight entries each, so that it is read once: the mean, then the squares about it, then the results.
+#include "cdl_block8.h"
+#include "cdl_chunks.h"
+
+namespace cdl {
+namespace {
+
+template <int L>
+constexpr int kThreadsOf = L > 256 ? L : 256;
+
+// Sums over the L lanes of a row, in all of them.  `slot` alternates between 0 and 1 from one sum to the next: beyond a wave, one barrier each.
+template <int L, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], int slot)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#define CDL_ROR(D) v[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v[i]), 0x120 + D, 0xf, 0xf, false))
+        CDL_ROR(8); CDL_ROR(4); CDL_ROR(2); CDL_ROR(1);
+#undef CDL_ROR
+        if (L >= 64) {
+            v[i] += __shfl_xor(v[i], 16, 64);
+            v[i] += __shfl_xor(v[i], 32, 64);
+        }
+    }
+    if constexpr (L > 64) {
+        __shared__ float sums[2][N][L / 64];
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) sums[slot][i][threadIdx.x >> 6] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < L / 64; ++w) v[i] += sums[slot][i][w];
+        }
+    }
+}
+
+struct NormFwd {
+    const void *x;
+    const float *weight, *bias;
+    int rows, cols;
+    float eps, by_cols;
+    void *y;
+    float *mean, *rstd;
+    uint8_t *q, *scale;
+    int64_t pitch_c, pitch_r, rows_end;      // rows_end: with q, rows up to whole blocks
+    bool stream;
+};
+
+template <class T, int L, int C, bool RAGGED, int KEEP>      // KEEP: 0 no copy, 1 E4M3, 2 E5M2
+__global__ __launch_bounds__(kThreadsOf<L>)
+void layer_norm_fwd_kernel(NormFwd a)
+{
+    constexpr int kTeams = kThreadsOf<L> / L;
+    const int lane = threadIdx.x % L, team = threadIdx.x / L;
+    float w[C][8], b[C][8];
+    int left[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * L + lane) * 8;
+        left[c] = a.cols - col;
+        load_vector<RAGGED>(a.weight ? a.weight + col : nullptr, left[c], 1.0f, w[c]);
+        load_vector<RAGGED>(a.bias ? a.bias + col : nullptr, left[c], 0.0f, b[c]);
+    }
+    const int64_t step = (int64_t)gridDim.x * kTeams;
+    int64_t row = (int64_t)blockIdx.x * kTeams + team;
+    Raw8<T> raw[C];
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) raw[c] = load_raw<RAGGED>((const T *)a.x + r * a.cols + (c * L + lane) * 8, left[c], a.stream);
+    };
+    if (row < a.rows) fetch(row);
+    for (; row < a.rows_end; row += step) {
+        if (row < a.rows) {
+            float v[C][8];
+#pragma unroll
+            for (int c = 0; c < C; ++c) unpack(raw[c], v[c]);
+            if (row + step < a.rows) fetch(row + step);
+            float sum[1] = {0.0f};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum[0] += v[c][k];
+            row_sums<L>(sum, 0);
+            const float mean = sum[0] * a.by_cols;
+            if (KEEP) {
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    uint32_t largest = 0;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) largest = max(largest, __float_as_uint(v[c][k]) & 0x7fffffffu);
+                    const uint32_t byte = scale_byte(row16_max(largest), KEEP == 2 ? 15 : 8);
+                    const float by = inverse(byte);
+                    const int col = (c * L + lane) * 8;
+                    float s[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) s[k] = v[c][k] * by;
+                    if (col < a.pitch_c) {
+                        *reinterpret_cast<u32x2 *>(a.q + row * a.pitch_c + col) = eight<KEEP == 2>(s);
+                        if ((lane & 15) == 0) a.scale[(int64_t)(col >> 7) * a.pitch_r + row] = (uint8_t)byte;
+                    }
+                }
+            }
+            float square[1] = {0.0f};
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[c][k] = (RAGGED ? k < left[c] : left[c] > 0) ? v[c][k] - mean : 0.0f;
+                    square[0] = __builtin_fmaf(v[c][k], v[c][k], square[0]);
+                }
+            row_sums<L>(square, 1);
+            const float rstd = 1.0f / sqrtf(square[0] * a.by_cols + a.eps);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float y[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) y[k] = __builtin_fmaf(v[c][k] * rstd, w[c][k], b[c][k]);
+                store_first<RAGGED>((T *)a.y + row * a.cols + (c * L + lane) * 8, left[c], y, a.stream);
+            }
+            if (lane == 0) {
+                if (a.mean) a.mean[row] = mean;
+                if (a.rstd) a.rstd[row] = rstd;
+            }
+        } else if (KEEP) {      // scales of rows beyond the matrix
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int col = (c * L + lane) * 8;
+                if (col < a.pitch_c && (lane & 15) == 0) a.scale[(int64_t)(col >> 7) * a.pitch_r + row] = (uint8_t)kLeast;
+            }
+        }
+    }
+}
+
+struct NormBwd {
+    const void *g, *x;
+    const uint8_t *q, *scale;
+    const float *weight, *mean, *rstd;
+    const void *add;
+    int rows, cols;
+    float by_cols;
+    void *d_x;
+    float *parts;                      // [block][2][part_cols]: d_w, d_b of the block's rows; or null
+    int64_t pitch_c, pitch_r, part_cols;
+    bool stream;
+};
+
+// KEPT: 0 from x, 1 from its copy in E4M3, 2 E5M2
+template <class T, int L, int C, bool RAGGED, int KEPT>
+__global__ __launch_bounds__(kThreadsOf<L>)
+void layer_norm_bwd_kernel(NormBwd a)
+{
+    constexpr int kTeams = kThreadsOf<L> / L;
+    const int lane = threadIdx.x % L, team = threadIdx.x / L;
+    float w[C][8], dw[C][8], db[C][8];
+    int left[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * L + lane) * 8;
+        left[c] = a.cols - col;
+        load_vector<RAGGED>(a.weight ? a.weight + col : nullptr, left[c], 1.0f, w[c]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dw[c][k] = db[c][k] = 0.0f;
+    }
+    const int64_t step = (int64_t)gridDim.x * kTeams;
+    Raw8<T> raw_g[C], raw_x[C], raw_add[C];
+    u32x2 kept[C];
+    uint32_t byte[C];
+    float mean = 0.0f, rstd = 0.0f;
+    auto fetch = [&](int64_t r) {
+        mean = a.mean[r];
+        rstd = a.rstd[r];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * L + lane) * 8;
+            const int64_t at = r * a.cols + col;
+            raw_g[c] = load_raw<RAGGED>((const T *)a.g + at, left[c], a.stream);
+            if (KEPT) {
+                if (left[c] > 0) {
+                    kept[c] = *reinterpret_cast<const u32x2 *>(a.q + r * a.pitch_c + col);
+                    byte[c] = a.scale[(int64_t)(col >> 7) * a.pitch_r + r];
+                } else {
+                    kept[c] = u32x2{0, 0};
+                    byte[c] = 127;
+                }
+            } else {
+                raw_x[c] = load_raw<RAGGED>((const T *)a.x + at, left[c], a.stream);
+            }
+            if (a.add && a.d_x) raw_add[c] = load_raw<RAGGED>((const T *)a.add + at, left[c], a.stream);
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * kTeams + team;
+    if (row < a.rows) fetch(row);
+    int slot = 0;
+    for (; row < a.rows; row += step) {
+        float n[C][8], h[C][8], add[C][8];      // c, then h; g is in `add` till h is there
+        const float r = rstd;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (KEPT) {
+                values8<KEPT == 2>(kept[c], n[c]);
+                const float by = scale_of(byte[c]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) n[c][k] *= by;
+            } else {
+                unpack(raw_x[c], n[c]);
+            }
+            unpack(raw_g[c], h[c]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                n[c][k] = (n[c][k] - mean) * r;
+                dw[c][k] = __builtin_fmaf(h[c][k], n[c][k], dw[c][k]);
+                db[c][k] += h[c][k];
+                h[c][k] *= w[c][k];
+            }
+            if (a.add && a.d_x) unpack(raw_add[c], add[c]);
+            else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) add[c][k] = 0.0f;
+            }
+        }
+        if (row + step < a.rows) fetch(row + step);
+        if (!a.d_x) continue;
+        float sums[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                sums[0] += h[c][k];
+                sums[1] = __builtin_fmaf(h[c][k], n[c][k], sums[1]);
+            }
+        row_sums<L>(sums, slot);
+        slot ^= 1;
+        const float one = sums[0] * a.by_cols, two = sums[1] * a.by_cols;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float d[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) d[k] = __builtin_fmaf(h[c][k] - one - n[c][k] * two, r, add[c][k]);
+            store_first<RAGGED>((T *)a.d_x + row * a.cols + (c * L + lane) * 8, left[c], d, a.stream);
+        }
+    }
+    if (!a.parts) return;
+    float *const out = a.parts + (int64_t)blockIdx.x * 2 * a.part_cols;
+    if constexpr (kTeams > 1) {      // the teams of a block one after the other
+        __shared__ float part[2][L * C * 8];
+        for (int t = 0; t < kTeams; ++t) {
+            if (team == t) {
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int at = (c * L + lane) * 8 + k;
+                        part[0][at] = t ? part[0][at] + dw[c][k] : dw[c][k];
+                        part[1][at] = t ? part[1][at] + db[c][k] : db[c][k];
+                    }
+            }
+            __syncthreads();
+        }
+        for (int at = threadIdx.x; at < a.part_cols; at += kThreadsOf<L>) {
+            out[at] = part[0][at];
+            out[a.part_cols + at] = part[1][at];
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * L + lane) * 8;
+            if (col < a.part_cols) {
+                store8(out + col, dw[c], false);
+                store8(out + a.part_cols + col, db[c], false);
+            }
+        }
+    }
+}
+
+constexpr int kForms = 8;
+// lanes of a row, chunks of a lane: up to 128, 256, 512, 1024, 2048, 4096, 8192 and 32768 entries
+constexpr int kLanes[kForms] = {16, 16, 64, 64, 256, 256, 256, 1024}, kChunksOf[kForms] = {1, 2, 1, 2, 1, 2, 4, 4};
+int form_of(int32_t cols)
+{
+    int f = 0;
+    while (f < kForms - 1 && cols > kLanes[f] * kChunksOf[f] * 8) ++f;
+    return f;
+}
+int64_t teams_of(int form) { return (kLanes[form] > 256 ? kLanes[form] : 256) / kLanes[form]; }
+
+int64_t fwd_blocks(int form, int64_t rows)
+{
+    const int64_t blocks = (rows + teams_of(form) - 1) / teams_of(form), most = kLanes[form] > 256 ? 512 : 2048;
+    return blocks < most ? blocks : most;
+}
+int64_t bwd_blocks(int form, int64_t rows)
+{
+    const int64_t blocks = (rows + teams_of(form) - 1) / teams_of(form), most = kLanes[form] > 256 ? 256 : 1024;
+    return blocks < most ? blocks : most;
+}
+int64_t part_cols(int32_t cols) { return ((int64_t)cols + 7) / 8 * 8; }
+
+template <class T, bool RAGGED, int KEEP>
+int launch_fwd(const NormFwd &a, hipStream_t stream)
+{
+    const int form = form_of(a.cols);
+    typedef void (*kernel_t)(NormFwd);
+    static const kernel_t kernels[kForms] = {layer_norm_fwd_kernel<T, 16, 1, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 16, 2, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 64, 1, RAGGED, KEEP>,
+                                             layer_norm_fwd_kernel<T, 64, 2, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 256, 1, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 256, 2, RAGGED, KEEP>,
+                                             layer_norm_fwd_kernel<T, 256, 4, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 1024, 4, RAGGED, KEEP>};
+    CDL_LAUNCH("layer_norm_fwd_kernel", stream, kernels[form], dim3((unsigned)fwd_blocks(form, a.rows_end)), dim3(kLanes[form] > 256 ? kLanes[form] : 256), 0, a);
+    return check_launch();
+}
+template <class T>
+int launch_fwd(const NormFwd &a, int keep, hipStream_t stream)
+{
+    if (a.cols % 8 == 0) return keep == 0 ? launch_fwd<T, false, 0>(a, stream) : keep == 1 ? launch_fwd<T, false, 1>(a, stream) : launch_fwd<T, false, 2>(a, stream);
+    return keep == 0 ? launch_fwd<T, true, 0>(a, stream) : keep == 1 ? launch_fwd<T, true, 1>(a, stream) : launch_fwd<T, true, 2>(a, stream);
+}
+
+template <class T, bool RAGGED, int KEPT>
+int launch_bwd(const NormBwd &a, hipStream_t stream)
+{
+    const int form = form_of(a.cols);
+    typedef void (*kernel_t)(NormBwd);
+    static const kernel_t kernels[kForms] = {layer_norm_bwd_kernel<T, 16, 1, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 16, 2, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 64, 1, RAGGED, KEPT>,
+                                             layer_norm_bwd_kernel<T, 64, 2, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 256, 1, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 256, 2, RAGGED, KEPT>,
+                                             layer_norm_bwd_kernel<T, 256, 4, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 1024, 4, RAGGED, KEPT>};
+    CDL_LAUNCH("layer_norm_bwd_kernel", stream, kernels[form], dim3((unsigned)bwd_blocks(form, a.rows)), dim3(kLanes[form] > 256 ? kLanes[form] : 256), 0, a);
+    return check_launch();
+}
+template <class T>
+int launch_bwd(const NormBwd &a, int kept, hipStream_t stream)
+{
+    if (a.cols % 8 == 0) return kept == 0 ? launch_bwd<T, false, 0>(a, stream) : kept == 1 ? launch_bwd<T, false, 1>(a, stream) : launch_bwd<T, false, 2>(a, stream);
+    return kept == 0 ? launch_bwd<T, true, 0>(a, stream) : kept == 1 ? launch_bwd<T, true, 1>(a, stream) : launch_bwd<T, true, 2>(a, stream);
+}
+
+}  // namespace
+
+int launch_layer_norm_fwd(const void *x, int32_t type, const float *weight, const float *bias, int32_t rows, int32_t cols, float eps, void *y, float *mean, float *rstd,
+                          uint8_t *q, uint8_t *scale, int32_t format, hipStream_t stream)
+{
+    if (rows == 0) return CDL_OK;
+    const int64_t size = type == CDL_BF16 ? 2 : 4;
+    const NormFwd a{x, weight, bias, rows, cols, eps, 1.0f / (float)cols, y, mean, rstd, q, scale, block8_pitch(cols), block8_pitch(rows), q ? block8_pitch(rows) : rows,
+                    (int64_t)rows * cols * size >= kStreamFrom * 4};
+    const int keep = !q ? 0 : format == CDL_E5M2 ? 2 : 1;
+    return type == CDL_BF16 ? launch_fwd<bf16_t>(a, keep, stream) : launch_fwd<float>(a, keep, stream);
+}
+
+size_t layer_norm_bwd_workspace_bytes(int32_t rows, int32_t cols)
+{
+    if (rows == 0) return 0;
+    return align_up((size_t)bwd_blocks(form_of(cols), rows) * 2 * (size_t)part_cols(cols) * sizeof(float), 256);
+}
+
+int launch_layer_norm_bwd(const void *g, int32_t type, const void *x, const uint8_t *q, const uint8_t *scale, int32_t format, const float *weight, const float *mean,
+                          const float *rstd, const void *add, int32_t rows, int32_t cols, void *d_x, float *d_weight, float *d_bias, void *ws, hipStream_t stream)
+{
+    float *const parts = d_weight || d_bias ? (float *)ws : nullptr;
+    const int64_t size = type == CDL_BF16 ? 2 : 4;
+    if (rows > 0) {
+        const NormBwd a{g, x, q, scale, weight, mean, rstd, add, rows, cols, 1.0f / (float)cols, d_x, parts, block8_pitch(cols), block8_pitch(rows), part_cols(cols),
+                        (int64_t)rows * cols * size >= kStreamFrom * 4};
+        const int kept = !q ? 0 : format == CDL_E5M2 ? 2 : 1;
+        const int rc = type == CDL_BF16 ? launch_bwd<bf16_t>(a, kept, stream) : launch_bwd<float>(a, kept, stream);
+        if (rc != CDL_OK) return rc;
+    }
+    if (!d_weight && !d_bias) return CDL_OK;
+    return launch_column_sums(parts, rows > 0 ? bwd_blocks(form_of(cols), rows) : 0, cols, part_cols(cols), d_weight, d_bias, stream);
+}
+
+}  // namespace cdl

@@ -190,6 +190,22 @@ wrong:
     X(cdl_head_loss_bwd, "ppippppiiippws",                                                                                              \
       (a.p[0], a.p[1], a.i[0], a.p[2], a.p[3], a.p[4], a.p[5], a.i[1], a.i[2], a.i[3], a.p[6], a.p[7], a.ws, a.ws_bytes, a.stream))     \
     X(cdl_dropout, "ppinruups", (a.p[0], a.p[1], a.i[0], a.n, a.f[0], a.u[0], a.u[1], a.p[2], a.stream))                                \
+    X(cdl_layer_norm_fwd, "pippiirpppppis",                                                                                             \
+      (a.p[0], a.i[0], a.p[1], a.p[2], a.i[1], a.i[2], a.f[0], a.p[3], a.p[4], a.p[5], a.p[6], a.p[7], a.i[3], a.stream))               \
+    X(cdl_layer_norm_bwd, "pipppippppiipppws",                                                                                          \
+      (a.p[0], a.i[0], a.p[1], a.p[2], a.p[3], a.i[1], a.p[4], a.p[5], a.p[6], a.p[7], a.i[2], a.i[3], a.p[8], a.p[9], a.p[10], a.ws,   \
+       a.ws_bytes, a.stream))                                                                                                           \
+    X(cdl_block8_gemm_act, "ppppiiiiipipppiws",                                                                                         \
+      (a.p[0], a.p[1], a.p[2], a.p[3], a.i[0], a.i[1], a.i[2], a.i[3], a.i[4], a.p[4], a.i[5], a.p[5], a.p[6], a.p[7], a.i[6], a.ws,    \
+       a.ws_bytes, a.stream))                                                                                                           \
+    X(cdl_block8_gemm_gated, "ppppppiiiiippipppiws",                                                                                    \
+      (a.p[0], a.p[1], a.p[2], a.p[3], a.p[4], a.p[5], a.i[0], a.i[1], a.i[2], a.i[3], a.i[4], a.p[6], a.p[7], a.i[5], a.p[8], a.p[9],  \
+       a.p[10], a.i[6], a.ws, a.ws_bytes, a.stream))                                                                                    \
+    X(cdl_act_bwd, "pipppiiiipppws",                                                                                                    \
+      (a.p[0], a.i[0], a.p[1], a.p[2], a.p[3], a.i[1], a.i[2], a.i[3], a.i[4], a.p[4], a.p[5], a.p[6], a.ws, a.ws_bytes, a.stream))     \
+    X(cdl_gated_bwd, "pippppppiiiipppppws",                                                                                             \
+      (a.p[0], a.i[0], a.p[1], a.p[2], a.p[3], a.p[4], a.p[5], a.p[6], a.i[1], a.i[2], a.i[3], a.i[4], a.p[7], a.p[8], a.p[9],          \
+       a.p[10], a.p[11], a.ws, a.ws_bytes, a.stream))                                                                                   \
     /* the last integer: whether the weight quantizer is given */                                                                       \
     X(cdl_qgemm_bwd_quantize_bwd, "pppiiipqfopppppiqpppws",                                                                             \
       (a.p[0], a.p[1], a.p[2], a.i[0], a.i[1], a.i[2], a.p[3], &a.q[0], a.f[0], a.i[3], a.p[4], a.p[5], a.p[6], a.p[7], a.p[8],         \

@@ -1,0 +1,162 @@
+"""The backward passes of activations and of gated products against their formulas in 64 bits, from tensors and from their rows in eight bits."""
+import math
+
+import pytest
+
+import gpu_util as gu
+import sublayer_util as su
+
+pytestmark = pytest.mark.gpu
+KINDS = ("float32", "bfloat16")
+SIZES = [(1, 1), (1, 1000), (2, 7), (5, 8), (16, 256), (17, 257), (100, 130), (333, 1000), (1000, 2049), (4099, 520), (20000, 24), (3, 70001)]
+
+
+@pytest.fixture(scope="module")
+def env():
+    import paper_2501_09849_amd as cdl
+    return gu.torch_mod(), cdl
+
+
+def inputs(torch, rows, cols, kind, sides, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed + 31 * rows + cols)
+    make = lambda by: (torch.randn((rows, cols), device="cuda", generator=gen) * by).to(getattr(torch, kind))      # noqa: E731
+    return make(1.0), [make(2.0) for _ in range(sides)]
+
+
+def call(torch, cdl, g, sides, name, want="dby", fmt="e4m3", **given):
+    rows, cols = g.shape
+    new = lambda: torch.full_like(g, float("nan"))      # noqa: E731
+    vector = lambda: torch.full((cols,), float("nan"), device="cuda")      # noqa: E731
+    bytes_ = (cdl.act_bwd_workspace_bytes if sides == 1 else cdl.gated_bwd_workspace_bytes)(rows, cols)
+    ws = torch.full((max(256, bytes_),), 0xff, dtype=torch.uint8, device="cuda")
+    d, bias, y = [new() if "d" in want else None for _ in range(sides)], [vector() if "b" in want else None for _ in range(sides)], new() if "y" in want else None
+    number, kind = su.number(cdl, name), cdl.E5M2 if fmt == "e5m2" else cdl.E4M3
+    if sides == 1:
+        cdl.cdl_act_bwd(g, rows, cols, number, d_z=d[0], d_bias=bias[0], y=y, ws=ws, format=kind, **given)
+    else:
+        cdl.cdl_gated_bwd(g, rows, cols, number, d_gate=d[0], d_up=d[1], d_bias_gate=bias[0], d_bias_up=bias[1], y=y, ws=ws, format=kind, **given)
+    torch.cuda.synchronize()
+    return d, bias, y
+
+
+def given_of(sides, z=None, kept=None):
+    names = [""] if sides == 1 else ["_gate", "_up"]
+    if z is not None:
+        return {"z" + n: t for n, t in zip(names, z)}
+    return {k + n: t for n, pair in zip(names, kept) for k, t in zip(("q", "scale"), pair)}
+
+
+def check(torch, got, g, z, name, kind):
+    d, bias, y = got
+    wants, want_y = su.act_back(torch, name, g.double(), z, kind)
+    for i, (want, off) in enumerate(wants):
+        assert su.outside(d[i], want, off + su.HALF[kind] * want.abs()) == 0, i
+        assert su.outside(bias[i], *su.column_sum(torch, want, off)) == 0, i
+    assert su.outside(y, *want_y) == 0
+
+
+@pytest.mark.parametrize("name", su.ACTS)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("sides", [1, 2])
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_gradients(env, rows, cols, sides, kind, name):
+    torch, cdl = env
+    g, z = inputs(torch, rows, cols, kind, sides, 1)
+    got = call(torch, cdl, g, sides, name, **given_of(sides, z=z))
+    check(torch, got, g, [t.double() for t in z], name, kind)
+    again = call(torch, cdl, g, sides, name, **given_of(sides, z=z))
+    assert all(torch.equal(p, q) for a, b in zip(got[:2], again[:2]) for p, q in zip(a, b)) and torch.equal(got[2], again[2])
+    kept = [su.quantize(torch, cdl, t) for t in z]
+    check(torch, call(torch, cdl, g, sides, name, **given_of(sides, kept=kept)), g, [su.values(torch, q, s, "e4m3", cols) for q, s in kept], name, kind)
+
+
+@pytest.mark.parametrize("sides", [1, 2])
+def test_the_wider_format(env, sides):
+    torch, cdl = env
+    g, z = inputs(torch, 77, 300, "bfloat16", sides, 2)
+    kept = [su.quantize(torch, cdl, t, "e5m2") for t in z]
+    check(torch, call(torch, cdl, g, sides, "silu", fmt="e5m2", **given_of(sides, kept=kept)), g, [su.values(torch, q, s, "e5m2", 300) for q, s in kept], "silu", "bfloat16")
+
+
+@pytest.mark.parametrize("sides", [1, 2])
+def test_each_output_alone(env, sides):
+    torch, cdl = env
+    g, z = inputs(torch, 130, 300, "bfloat16", sides, 3)
+    all_ = call(torch, cdl, g, sides, "gelu", **given_of(sides, z=z))
+    assert all(torch.equal(p, q) for p, q in zip(call(torch, cdl, g, sides, "gelu", want="d", **given_of(sides, z=z))[0], all_[0]))
+    assert all(torch.equal(p, q) for p, q in zip(call(torch, cdl, g, sides, "gelu", want="b", **given_of(sides, z=z))[1], all_[1]))
+    assert torch.equal(call(torch, cdl, g, sides, "gelu", want="y", **given_of(sides, z=z))[2], all_[2])
+    if sides == 2:      # one bias, one gradient
+        up = torch.full((300,), 7.0, device="cuda")
+        ws = torch.empty(cdl.gated_bwd_workspace_bytes(130, 300), dtype=torch.uint8, device="cuda")
+        cdl.cdl_gated_bwd(g, 130, 300, cdl.ACT_GELU, d_bias_up=up, z_gate=z[0], z_up=z[1], ws=ws)
+        assert torch.equal(up, all_[1][1])
+
+
+@pytest.mark.parametrize("name", su.ACTS)
+def test_the_whole_range_of_z(env, name):
+    """Values and derivatives from -300 to 300, at zero of either sign, and what is not finite in its own entry alone."""
+    torch, cdl = env
+    z = torch.cat([torch.linspace(-300, 300, 4001), torch.linspace(-12, 12, 8193), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 1e30, -1e30]), 2.0 ** -torch.arange(0, 120.0)]).cuda()[None]
+    g = torch.ones_like(z)
+    d, _, y = call(torch, cdl, g, 1, name, want="dy", z=z)
+    (want, off), = su.act_back(torch, name, g.double(), [z.double()], "float32")[0]
+    want_y, off_y = su.act_back(torch, name, g.double(), [z.double()], "float32")[1]
+    assert su.outside(d[0], want, off + su.U * want.abs()) == 0 and su.outside(y, want_y, off_y) == 0
+    z[0, 7], z[0, 100], z[0, 200] = float("nan"), float("inf"), -float("inf")
+    d2, _, y2 = call(torch, cdl, g, 1, name, want="dy", z=z)
+    keep = torch.ones_like(z, dtype=torch.bool)
+    keep[0, [7, 100, 200]] = False
+    assert torch.equal(d2[0][keep], d[0][keep]) and torch.equal(y2[keep], y[keep])
+    assert math.isnan(float(y2[0, 7])) and math.isnan(float(d2[0][0, 7])) == (name != "none") and float(y2[0, 100]) == float("inf")      # (1 whatever z is)
+
+
+@pytest.mark.parametrize("name", ["gelu", "silu"])
+def test_derivatives_are_those_of_differences(env, name):
+    torch, cdl = env
+    z = torch.linspace(-6, 6, 2001, device="cuda", dtype=torch.float64).float()[None]
+    d, _, _ = call(torch, cdl, torch.ones_like(z), 1, name, want="d", z=z)
+    f = lambda e: su.act(torch, name, z.double() + e)[0]      # noqa: E731
+    h = 1e-3
+    want = (8 * (f(h) - f(-h)) - (f(2 * h) - f(-2 * h))) / (12 * h)      # the fifth derivative's share, below 10 h^4 / 30, and roundings
+    assert float((d[0].double() - want).abs().max()) < 2e-6
+
+
+@pytest.mark.parametrize("sides", [1, 2])
+def test_a_block_that_is_not_finite(env, sides):
+    torch, cdl = env
+    g, z = inputs(torch, 20, 300, "bfloat16", sides, 4)
+    kept = [su.quantize(torch, cdl, t) for t in z]
+    clean = call(torch, cdl, g, sides, "silu", **given_of(sides, kept=kept))
+    z[0][3, 200] = float("inf")
+    kept[0] = su.quantize(torch, cdl, z[0])
+    got = call(torch, cdl, g, sides, "silu", **given_of(sides, kept=kept))
+    hit = torch.zeros((20, 300), dtype=torch.bool, device="cuda")
+    hit[3, 128:256] = True
+    for p, q in zip(got[0] + [got[2]], clean[0] + [clean[2]]):
+        assert torch.isnan(p[hit]).all() and torch.equal(p[~hit], q[~hit])
+
+
+@pytest.mark.parametrize("sides", [1, 2])
+def test_in_place(env, sides):
+    torch, cdl = env
+    for cols in (300, 301):
+        g, z = inputs(torch, 100, cols, "bfloat16", sides, 5)
+        d, _, y = call(torch, cdl, g, sides, "silu", **given_of(sides, z=z))
+        if sides == 1:
+            own, t = g.clone(), z[0].clone()
+            cdl.cdl_act_bwd(own, 100, cols, cdl.ACT_SILU, d_z=own, y=t, z=t)
+            assert torch.equal(own, d[0]) and torch.equal(t, y)
+        else:
+            own, t = g.clone(), [v.clone() for v in z]
+            cdl.cdl_gated_bwd(own, 100, cols, cdl.ACT_SILU, d_gate=t[0], d_up=t[1], y=own, z_gate=t[0], z_up=t[1])
+            assert torch.equal(t[0], d[0]) and torch.equal(t[1], d[1]) and torch.equal(own, y)
+
+
+def test_no_rows(env):
+    torch, cdl = env
+    b = [torch.full((5,), 7.0, device="cuda") for _ in range(3)]
+    cdl.cdl_act_bwd(None, 0, 5, cdl.ACT_GELU, d_bias=b[0], type=cdl.F32)
+    cdl.cdl_gated_bwd(None, 0, 5, cdl.ACT_GELU, d_bias_gate=b[1], d_bias_up=b[2], type=cdl.BF16)
+    assert all((v == 0).all() for v in b)
+    cdl.cdl_act_bwd(None, 5, 0, cdl.ACT_GELU, d_bias=b[0], type=cdl.F32)

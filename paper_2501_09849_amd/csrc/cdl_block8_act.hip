@@ -1,7 +1,7 @@
 // The block-scaled product with what stands behind it in a layer, and the gated product of two projections:
 //
 //   z = a b^T + bias,  y = act(z) + add                    y = act(a gate^T + bias) * (a up^T + bias)
-#include "cdl_act.h"
+#include "cdl_act_thin.h"
 #include "cdl_chunks.h"
 
 namespace cdl {
@@ -73,15 +73,100 @@ int launch_finish(const Finish &f, int act, bool gated, hipStream_t stream)
     return gated ? launch_finish<T, true, true>(f, act, stream) : launch_finish<T, false, true>(f, act, stream);
 }
 
+// How a product is formed: in fp32 through memory, its contraction in parts; in tiles of 256 x 256, or of 128 x 128 two to a compute unit, finished from the accumulators;
+// or by blocks of 16 rows of the weights.
+enum Way { kParts, kWide, kPair, kThin };
+struct Choice {
+    Way way;
+    int rows;      // kThin: rows of a, in sixteens
+};
+
+// The way that takes least, in us.  A K-tile of 256 x 256 takes 1.72 us (from fp8 in the exact instructions 3.2), one of 128 x 128 1.0 with another block beside it and 0.7 alone
+// (1.8, 1.2); the epilogue of a tile 7 us and 3.5, with gelu 15 and 4.5: the two blocks of a compute unit share the time that one would wait for the other's.  Thin blocks read their rows from L2 at 8 MB
+// a us, behind the latency of a wave's own K-tiles.  Measured, us, as Parts, Wide, Pair, Thin:
+//   4 x 4096 x 1024 gelu            9.5     -     11.1   5.3         1 x 2048 x 768 gated            15.1     -      8.4    5.8
+//   64 x 4096 x 4096 gelu          16.3     -     26.7  12.7         128 x 4096 x 4096 gelu          16.5     -     27.4   23.6
+//   300 x 400 x 9000 gelu          13.5     -     52.8  15.4         1000 x 4096 x 1024 gelu         23.2   32.4    13.6    -
+//   2048 x 2048 x 2048             23.0   31.9    15.7   -           65536 x 4096 x 768               602    293     336    -
+//   65536 x 4096 x 768 gelu         609    417     370   -           65536 x 2048 x 768 gated, z kept 687    371     392    -
+//   32768 x 4096 x 768 gated, fp32  744    433     459   -           32768 x 4096 x 768, fp32         436  (423)     272    -
+float ring_us(bool wide, bool gated, bool exact, int32_t M, int32_t N, int nk, int act)
+{
+    const int p = (wide ? 256 : 128) / (gated ? 2 : 1), q = wide ? 256 : 128, places = wide ? 256 : 512;
+    const int64_t tiles = (((int64_t)N + p - 1) / p) * (((int64_t)M + q - 1) / q), rounds = (tiles + places - 1) / places;
+    const float tile = wide ? (exact ? 3.2f : 1.72f) : tiles <= 256 ? (exact ? 1.2f : 0.7f) : exact ? 1.8f : 1.0f;
+    const float end = wide ? (act == CDL_ACT_GELU ? 15.0f : 7.0f) : act == CDL_ACT_GELU ? 4.5f : 3.5f;
+    return 4.0f + (float)rounds * ((float)nk * tile + end);
+}
+Choice choose(int32_t M, int32_t N, int32_t K, bool gated, int y_type, int act)
+{
+    if (K == 0) return {kParts, 0};
+    const bool exact = y_type == CDL_F32;
+    const int nk = (int)(block8_pitch(K) / kRingRow);
+    Choice best{kParts, 0};
+    float least = block8_parts_us(M, N, K) * (gated ? 2.0f : 1.0f) * (exact ? 1.5f : 1.0f);
+    for (const bool wide : {false, true}) {
+        if (wide && exact && !gated) continue;
+        const float us = ring_us(wide, gated, exact, M, N, nk, act);
+        if (us < least) {
+            least = us;
+            best.way = wide ? kWide : kPair;
+        }
+    }
+    for (const int rows : {1, 2, 4}) {
+        const int64_t across = ((int64_t)M + 16 * rows - 1) / (16 * rows), blocks = ((int64_t)N + 15) / 16 * across;
+        const float read = (float)((gated ? 2 : 1) + rows);      // sixteens of a block
+        const float us = 4.0f + (float)blocks * 16.0f * read * (float)block8_pitch(K) / 8e6f + 0.2f * read * (float)((nk + 7) / 8) + 2.0f * (float)(blocks / 512);
+        if (us < least && across <= 65535) {
+            least = us;
+            best = {kThin, rows};
+        }
+    }
+    return best;
+}
+
 size_t parts_bytes(int32_t M, int32_t N, int32_t K) { return align_up((size_t)block8_parts(M, N, K) * (size_t)M * (size_t)N * sizeof(float), 256); }
 
 }  // namespace
 
-size_t block8_gemm_act_workspace_bytes(int32_t M, int32_t N, int32_t K, bool gated) { return parts_bytes(M, N, K) * (gated ? 2 : 1); }
+size_t block8_gemm_act_workspace_bytes(int32_t M, int32_t N, int32_t K, bool gated)
+{
+    if (M == 0 || N == 0 || K == 0) return 0;
+    // (whatever the results' type and the activation, which the query does not know)
+    for (const int type : {CDL_BF16, CDL_F32})
+        for (const int act : {CDL_ACT_NONE, CDL_ACT_GELU})
+            if (choose(M, N, K, gated, type, act).way == kParts) return parts_bytes(M, N, K) * (gated ? 2 : 1);
+    return 0;
+}
 
 int launch_block8_gemm_act(const ProductCall &c, bool gated, hipStream_t stream)
 {
     if (c.M == 0 || c.N == 0) return CDL_OK;
+    const ActTarget to{{c.bias[0], c.bias[1]}, c.add, c.y, {c.z[0], c.z[1]}, c.M, c.N, c.act};
+    const int64_t ld = block8_pitch(c.K), pitch_a = block8_pitch(c.M), pitch_b = block8_pitch(c.N);
+    const int nk = (int)(ld / kRingRow);
+    const Choice choice = choose(c.M, c.N, c.K, gated, c.y_type, c.act);
+    if (choice.way == kThin)
+        return launch_thin_any({c.a, {c.b[0], c.b[1]}, c.a_scale, {c.b_scale[0], c.b_scale[1]}, ld, pitch_a, pitch_b, nk, to}, choice.rows, gated, c.y_type, c.a_format, c.b_format,
+                               stream);
+    if (choice.way != kParts) {
+        RingJob job{};
+        job.P = c.b[0];
+        job.P2 = c.b[1];
+        job.Q = c.a;
+        job.ldp = job.ldq = ld;
+        job.rowsP = c.N;
+        job.rowsQ = c.M;
+        job.nk = job.k_per = nk;
+        job.splits = 1;
+        job.sp = c.b_scale[0];
+        job.sp2 = c.b_scale[1];
+        job.sq = c.a_scale;
+        job.pitch_sp = pitch_b;
+        job.pitch_sq = pitch_a;
+        const auto launch = c.y_type == CDL_BF16 ? (gated ? launch_gated_bf16 : launch_act_bf16) : gated ? launch_gated_f32 : launch_act_f32;
+        return launch(choice.way == kWide, job, to, c.a_format, c.b_format, stream);
+    }
     Finish f{};
     f.splits = block8_parts(c.M, c.N, c.K);
     f.M = c.M;

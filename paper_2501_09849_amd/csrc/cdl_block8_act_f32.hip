@@ -1,0 +1,11 @@
+// The tiles with an activation of the block-scaled product, results in fp32.
+#include "cdl_act_ring.h"
+
+namespace cdl {
+
+int launch_act_f32(bool wide, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream)
+{
+    return launch_act_ring<false, float>(wide, job, to, a_format, b_format, stream);
+}
+
+}  // namespace cdl

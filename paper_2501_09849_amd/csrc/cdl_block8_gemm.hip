@@ -191,6 +191,11 @@ int launch_block8_gemm(const uint8_t *a, const uint8_t *a_scale, const uint8_t *
 
 // The product as fp32 sums of the parts of the contraction, parts[split][M][N], for a kernel that adds them up.
 int block8_parts(int32_t M, int32_t N, int32_t K) { return M == 0 || N == 0 || K == 0 ? 0 : layout(M, N, K).splits; }
+float block8_parts_us(int32_t M, int32_t N, int32_t K)
+{
+    const Layout l = layout(M, N, K);
+    return 0.6f * (l.cost + (l.splits > 1 ? 0.0f : 13.0f + (float)M * (float)N * 2.7e-6f));
+}
 int launch_block8_parts(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale, int32_t M, int32_t N, int32_t K, int32_t a_format,
                         int32_t b_format, bool exact, float *parts, hipStream_t stream)
 {

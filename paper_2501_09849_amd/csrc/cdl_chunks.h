@@ -5,9 +5,6 @@
 
 namespace cdl {
 
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-
 template <class T> struct Raw8;
 template <> struct Raw8<bf16_t> { u32x4 a; };
 template <> struct Raw8<float> { f32x4 a, b; };

@@ -239,6 +239,7 @@ int launch_head_loss_bwd(const void *h, const void *w, int32_t type, const int64
 int launch_dropout(const void *x, const void *add, int32_t type, int64_t n, float p, uint64_t seed, uint64_t counter, void *y, hipStream_t stream);      // (cdl_dropout.hip)
 
 int block8_parts(int32_t M, int32_t N, int32_t K);      // parts of the contraction, 0 where there is nothing to multiply
+float block8_parts_us(int32_t M, int32_t N, int32_t K);      // about what they and a kernel that adds them up take
 int launch_block8_parts(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale, int32_t M, int32_t N, int32_t K, int32_t a_format,
                         int32_t b_format, bool exact, float *parts, hipStream_t stream);
 

@@ -32,18 +32,22 @@ constexpr int wait_imm(int vm) { return (vm & 15) | ((vm >> 4) << 14) | 0x0070; 
 
 // WP x WQ waves of TP x TQ accumulators; NP, NQ: K-tiles of each operand in LDS; STAGING: LDS bytes in which a wave turns its results into rows, 0: in the slot of P
 // that is free then; SCALES: a byte for every row comes with a K-tile.
+// GATED: P is two matrices of the same shape, and a tile holds half as many entries of either, side by side for each wave: of a wave's accumulators along P the first half
+// are of the first matrix, the others of the same entries of the second.
 // After a K-tile its slots are free.  The loads of Q into its slot go out with the last products of the K-tile, those of P with the first ones of the next K-tile
 // (behind a tile's results), or with those of Q where P has no third slot.
-template <int WP_, int WQ_, int TP_, int TQ_, int NP_, int NQ_, int PER_CU_, int STAGING_ = 0, bool SCALES_ = false>
+template <int WP_, int WQ_, int TP_, int TQ_, int NP_, int NQ_, int PER_CU_, int STAGING_ = 0, bool SCALES_ = false, bool GATED_ = false>
 struct RingForm {
     static constexpr int WP = WP_, WQ = WQ_, TP = TP_, TQ = TQ_, NP = NP_, NQ = NQ_, PER_CU = PER_CU_;
-    static constexpr bool SCALES = SCALES_, kTogether = NP == 2;
+    static constexpr bool SCALES = SCALES_, GATED = GATED_, kTogether = NP == 2;
     static constexpr int kWaves = WP * WQ, kThreads = 64 * kWaves, kP = WP * TP * 32, kQ = WQ * TQ * 32;
+    static constexpr int kAcross = GATED ? kP / 2 : kP, kWaveAcross = kAcross / WP;      // entries of the result along P of a tile, of a wave
     static constexpr int kSlotP = kP * kRingRow, kSlotQ = kQ * kRingRow, kScaleBytes = 256, kSlotS = SCALES ? 2 * kScaleBytes : 0;
     static constexpr int kAtQ = NP * kSlotP, kAtS = kAtQ + NQ * kSlotQ, kAtStaging = kAtS + NQ * kSlotS, kLds = kAtStaging + kWaves * STAGING_;
     static constexpr int kLoadsP = kP / 8 / kWaves, kLoadsQ = kQ / 8 / kWaves, kMoreQ = kLoadsQ + (SCALES ? 1 : 0);      // of a wave and K-tile, 1 KB each; and the scales
     static constexpr int STAGING = STAGING_ ? STAGING_ : kLoadsP * 1024;
     static_assert(kLoadsP * 8 * kWaves == kP && kLoadsQ * 8 * kWaves == kQ && (NP == NQ || NP == NQ + 1) && NQ >= 2, "whole loads; the order of the loads");
+    static_assert(!GATED || (WQ == 2 && TP % 2 == 0), "a wave's loads are of one matrix");
     static_assert(!kTogether || STAGING_ > 0, "a free slot of P between tiles");
     static_assert(PER_CU * kLds <= 160 << 10 && kP <= 256 && kQ <= 256 && kWaves % 2 == 0, "LDS; scales of an operand in one load");
 };
@@ -61,6 +65,7 @@ struct RingJob {
     const uint8_t *sp, *sq;        // scales: [K-tile][pitch], pitches multiples of 128
     int64_t pitch_sp, pitch_sq;
     int downP, downQ;              // rows in memory of an operand whose contraction runs down its rows
+    const uint8_t *P2, *sp2;       // GATED: the second matrix, its scales
     uint64_t by_tiles, by_group;   // 1 / (tiles_p tiles_q) and 1 / (4 tiles_p), of a launch: ring_ready()
 };
 
@@ -99,7 +104,7 @@ __device__ __forceinline__ RingUnit ring_unit(const RingJob &job, int unit)
     const int split = divide(unit, job.by_tiles), t = unit - split * job.tiles_p * job.tiles_q;
     const int group = divide(t, job.by_group), in = t - group * 4 * job.tiles_p, high = min(4, job.tiles_q - 4 * group);
     const int p = high == 4 ? in >> 2 : high == 3 ? (int)((uint32_t)in / 3u) : in >> (high - 1), q = 4 * group + in - p * high;
-    return {p * FORM::kP, q * FORM::kQ, split};
+    return {p * FORM::kAcross, q * FORM::kQ, split};
 }
 
 struct OpBf16 {
@@ -187,6 +192,7 @@ struct OpF8 {
 template <class FORM, bool PLANES, bool IS_P, bool DOWN>
 struct RingStream {
     static constexpr int kLoads = IS_P ? FORM::kLoadsP : FORM::kLoadsQ, kBack = 4096;      // (offsets stay positive)
+    static constexpr bool kGated = FORM::GATED && IS_P;
     static constexpr int kEntries = IS_P ? FORM::kP : FORM::kQ, kChunks = kEntries / 8, kRows = 64 / kChunks;      // DOWN: 16-byte chunks of a row, rows of a load
     int unit, left, end, product, rows_in;
     const uint8_t *src, *src_s;
@@ -234,15 +240,15 @@ struct RingStream {
         step = 64 * ld;
         const int64_t at = DOWN ? (int64_t)row0 * 2 + in_plane * step : (int64_t)row0 * ld + (int64_t)in_plane * kRingRow;
         const int64_t rest = DOWN ? (IS_P ? job.downP : job.downQ) * ld - 16 - at : 0;
-        const uint8_t *const src = (IS_P ? job.P : job.Q) + at + (PLANES ? part(product) * (IS_P ? job.plane_p : job.plane_q) : 0) - kBack;
-        const int most = DOWN ? 0 : min(rows - 1 - row0, kEntries - 1);
+        const uint8_t *const src = (kGated && (wave & 1) ? job.P2 : IS_P ? job.P : job.Q) + at + (PLANES ? part(product) * (IS_P ? job.plane_p : job.plane_q) : 0) - kBack;
+        const int most = DOWN ? 0 : min(rows - 1 - row0, kEntries - 1), from = kGated ? wave >> 1 : wave;      // GATED: even waves load the first matrix, odd ones the same rows of the second
         if (most != rows_in) {
             rows_in = most;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {      // load i fills LDS rows 8 n ... 8 n + 7, chunk c of a row at c ^ (row / 2); rows beyond the matrix: its last one again, whose results nobody stores
                 const int n = wave * kLoads + i, k = n * kRows + lane / kChunks;
                 if (DOWN) off[i] = (uint32_t)k * (uint32_t)ld + (uint32_t)(lane % kChunks ^ turned(k)) * 16 + kBack - (i & 3) * 1024;
-                else off[i] = (uint32_t)min(n * 8 + (lane >> 3), most) * (uint32_t)ld + (uint32_t)((lane & 7) ^ ((4 * n + (lane >> 4)) & 7)) * 16 + kBack - (i & 3) * 1024;
+                else off[i] = (uint32_t)min((from * kLoads + i) * 8 + (lane >> 3), most) * (uint32_t)ld + (uint32_t)((lane & 7) ^ ((4 * n + (lane >> 4)) & 7)) * 16 + kBack - (i & 3) * 1024;
             }
         }
         if (FORM::SCALES && !IS_P) {      // four bytes a lane; half of the waves load those of Q, the others those of P
@@ -251,6 +257,12 @@ struct RingStream {
             const int at = q ? u.q0 : u.p0;
             src_s = (q ? job.sq : job.sp) + at + (int64_t)kt * pitch;
             off_s = (uint32_t)min((int64_t)lane * 4, pitch - 4 - at);
+            if (FORM::GATED && !q) {      // a lane's four rows are of one matrix
+                constexpr int kRows = FORM::kP / FORM::kWaves;
+                const int part = lane * 4 / kRows;
+                off_s = (uint32_t)min((int64_t)(part >> 1) * kRows + lane * 4 % kRows, pitch - 4 - at);
+                if (part & 1) src_s += job.sp2 - job.sp;
+            }
             step_s = pitch;
         }
         return {src, left, product, rest};
@@ -511,7 +523,7 @@ __device__ __forceinline__ void ring(const RingCall<EPILOGUE> &call)
         uint8_t *const staging = ring_lds + (FORM::kTogether || FORM::kLds > FORM::kAtStaging ? FORM::kAtStaging + wave * FORM::STAGING : free_p + wave * FORM::kLoadsP * 1024);
         const RingCall<EPILOGUE> &then = again(call);
         const RingUnit u = ring_unit<FORM>(then.job, unit);
-        then.epilogue(acc, u.p0 + wp * TP * 32, u.q0 + wq * TQ * 32, u.split, staging, own);
+        then.epilogue(acc, u.p0 + wp * FORM::kWaveAcross, u.q0 + wq * TQ * 32, u.split, staging, own);
         stored = true;
         read(0, Zero{});      // (again: the fragments would take registers that the results need)
     }

@@ -12,6 +12,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+// ... from any address of a bf16 or fp32 entry, 16 bytes in one access
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // A grid holds fewer than 2^32 threads: what has more entries than that goes through in several launches, launch(first, count) for kLaunchThreads at a time.
 constexpr int64_t kLaunchThreads = 1ll << 31;

@@ -56,7 +56,7 @@ class Case:
 # single tokens, few rows, ragged tiles of every form, contractions of one block and split ones
 SIZES = [(1, 1, 1), (1, 128, 128), (1, 2048, 768), (4, 1000, 130), (16, 333, 2048), (17, 48, 300), (33, 129, 640), (64, 64, 64), (64, 260, 4096), (65, 127, 129), (70, 31, 100), (128, 128, 1024),
          (200, 72, 8000), (129, 1001, 384), (255, 257, 256), (512, 512, 512), (1021, 1000, 520), (1024, 770, 4096), (300, 401, 9000), (2000, 1999, 520), (3000, 3001, 200), (3900, 4090, 900),
-         (4096, 4098, 128), (2048, 2048, 640)]
+         (4096, 4098, 128), (2048, 2048, 640), (129, 250, 30001), (256, 256, 32768)]
 
 
 @pytest.mark.parametrize("kind", KINDS)

@@ -36,7 +36,7 @@ void act_bwd_kernel(ActBwd a)
     uint32_t byte[S];
     auto fetch = [&](int64_t r) {
         const int64_t at = r * a.cols + col;
-        raw_g = load_raw<RAGGED>((const T *)a.g + at, left, a.stream);
+        raw_g = load_raw<RAGGED>((const T *)a.g + at, left, a.stream, a.cols < 8);
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             if (KEPT) {
@@ -48,7 +48,7 @@ void act_bwd_kernel(ActBwd a)
                     byte[s] = 127;
                 }
             } else {
-                raw_z[s] = load_raw<RAGGED>((const T *)a.z[s] + at, left, a.stream);
+                raw_z[s] = load_raw<RAGGED>((const T *)a.z[s] + at, left, a.stream, a.cols < 8);
             }
         }
     };
@@ -61,7 +61,7 @@ void act_bwd_kernel(ActBwd a)
     if (row < end) fetch(row);
     for (; row < end; row += kGroups) {
         float g[8], z[S][8], d[S][8], y[8];
-        unpack(raw_g, g);
+        unpack<RAGGED>(raw_g, left, a.cols < 8, g);
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             if (KEPT) {
@@ -70,7 +70,7 @@ void act_bwd_kernel(ActBwd a)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) z[s][k] *= by;
             } else {
-                unpack(raw_z[s], z[s]);
+                unpack<RAGGED>(raw_z[s], left, a.cols < 8, z[s]);
             }
         }
         if (row + kGroups < end) fetch(row + kGroups);

@@ -27,7 +27,7 @@ void block8_finish_kernel(Finish f)
     const int64_t whole = (int64_t)f.M * f.N;
     float bias[S][8];
 #pragma unroll
-    for (int s = 0; s < S; ++s) load_vector<RAGGED>(f.bias[s] ? f.bias[s] + col : nullptr, left, 0.0f, bias[s]);
+    for (int s = 0; s < S; ++s) load_vector<RAGGED>(f.bias[s] ? f.bias[s] + col : nullptr, left, f.N < 8, 0.0f, bias[s]);
     for (int64_t row = (int64_t)(blockIdx.x / (unsigned)f.col_blocks) * kRows + threadIdx.x / kLanes; row < f.M; row += (int64_t)f.row_blocks * kRows) {
         const int64_t at = row * f.N + col;
         float z[S][8], y[8], add[8];
@@ -37,7 +37,7 @@ void block8_finish_kernel(Finish f)
             for (int k = 0; k < 8; ++k) z[s][k] = 0.0f;
             for (int i = 0; i < f.splits; ++i) {
                 float v[8];
-                unpack(load_raw<RAGGED>(f.parts[s] + i * whole + at, left, false), v);
+                unpack<RAGGED>(load_raw<RAGGED>(f.parts[s] + i * whole + at, left, false, f.N < 8), left, f.N < 8, v);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) z[s][k] += v[k];
             }
@@ -45,7 +45,7 @@ void block8_finish_kernel(Finish f)
             for (int k = 0; k < 8; ++k) z[s][k] += bias[s][k];
             if (f.z[s]) store_first<RAGGED>((T *)f.z[s] + at, left, z[s], false);
         }
-        if (f.add) unpack(load_raw<RAGGED>((const T *)f.add + at, left, false), add);
+        if (f.add) unpack<RAGGED>(load_raw<RAGGED>((const T *)f.add + at, left, false, f.N < 8), left, f.N < 8, add);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const float v = act_value<ACT>(z[0][k]);

@@ -244,7 +244,7 @@ int launch_block8_parts(const uint8_t *a, const uint8_t *a_scale, const uint8_t 
                         int32_t b_format, bool exact, float *parts, hipStream_t stream);
 
 // ---- a feed-forward sublayer ----------------------------------------------------------------
-constexpr int32_t kNormMostCols = 32768;
+constexpr int32_t kNormMostCols = 16384;
 int launch_layer_norm_fwd(const void *x, int32_t type, const float *weight, const float *bias, int32_t rows, int32_t cols, float eps, void *y, float *mean, float *rstd,
                           uint8_t *q, uint8_t *scale, int32_t format, hipStream_t stream);      // (cdl_layer_norm.hip)
 size_t layer_norm_bwd_workspace_bytes(int32_t rows, int32_t cols);

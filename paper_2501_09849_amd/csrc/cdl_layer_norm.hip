@@ -67,22 +67,22 @@ void layer_norm_fwd_kernel(NormFwd a)
     for (int c = 0; c < C; ++c) {
         const int col = (c * L + lane) * 8;
         left[c] = a.cols - col;
-        load_vector<RAGGED>(a.weight ? a.weight + col : nullptr, left[c], 1.0f, w[c]);
-        load_vector<RAGGED>(a.bias ? a.bias + col : nullptr, left[c], 0.0f, b[c]);
+        load_vector<RAGGED>(a.weight ? a.weight + col : nullptr, left[c], a.cols < 8, 1.0f, w[c]);
+        load_vector<RAGGED>(a.bias ? a.bias + col : nullptr, left[c], a.cols < 8, 0.0f, b[c]);
     }
     const int64_t step = (int64_t)gridDim.x * kTeams;
     int64_t row = (int64_t)blockIdx.x * kTeams + team;
     Raw8<T> raw[C];
     auto fetch = [&](int64_t r) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) raw[c] = load_raw<RAGGED>((const T *)a.x + r * a.cols + (c * L + lane) * 8, left[c], a.stream);
+        for (int c = 0; c < C; ++c) raw[c] = load_raw<RAGGED>((const T *)a.x + r * a.cols + (c * L + lane) * 8, left[c], a.stream, a.cols < 8);
     };
     if (row < a.rows) fetch(row);
     for (; row < a.rows_end; row += step) {
         if (row < a.rows) {
             float v[C][8];
 #pragma unroll
-            for (int c = 0; c < C; ++c) unpack(raw[c], v[c]);
+            for (int c = 0; c < C; ++c) unpack<RAGGED>(raw[c], left[c], a.cols < 8, v[c]);
             if (row + step < a.rows) fetch(row + step);
             float sum[1] = {0.0f};
 #pragma unroll
@@ -166,11 +166,12 @@ void layer_norm_bwd_kernel(NormBwd a)
     for (int c = 0; c < C; ++c) {
         const int col = (c * L + lane) * 8;
         left[c] = a.cols - col;
-        load_vector<RAGGED>(a.weight ? a.weight + col : nullptr, left[c], 1.0f, w[c]);
+        load_vector<RAGGED>(a.weight ? a.weight + col : nullptr, left[c], a.cols < 8, 1.0f, w[c]);
 #pragma unroll
         for (int k = 0; k < 8; ++k) dw[c][k] = db[c][k] = 0.0f;
     }
     const int64_t step = (int64_t)gridDim.x * kTeams;
+    constexpr bool kAhead = L <= 256;      // the next row's loads under way while a row is worked on, as far as there are registers
     Raw8<T> raw_g[C], raw_x[C], raw_add[C];
     u32x2 kept[C];
     uint32_t byte[C];
@@ -182,7 +183,7 @@ void layer_norm_bwd_kernel(NormBwd a)
         for (int c = 0; c < C; ++c) {
             const int col = (c * L + lane) * 8;
             const int64_t at = r * a.cols + col;
-            raw_g[c] = load_raw<RAGGED>((const T *)a.g + at, left[c], a.stream);
+            raw_g[c] = load_raw<RAGGED>((const T *)a.g + at, left[c], a.stream, a.cols < 8);
             if (KEPT) {
                 if (left[c] > 0) {
                     kept[c] = *reinterpret_cast<const u32x2 *>(a.q + r * a.pitch_c + col);
@@ -192,16 +193,17 @@ void layer_norm_bwd_kernel(NormBwd a)
                     byte[c] = 127;
                 }
             } else {
-                raw_x[c] = load_raw<RAGGED>((const T *)a.x + at, left[c], a.stream);
+                raw_x[c] = load_raw<RAGGED>((const T *)a.x + at, left[c], a.stream, a.cols < 8);
             }
-            if (a.add && a.d_x) raw_add[c] = load_raw<RAGGED>((const T *)a.add + at, left[c], a.stream);
+            if (kAhead && a.add && a.d_x) raw_add[c] = load_raw<RAGGED>((const T *)a.add + at, left[c], a.stream, a.cols < 8);
         }
     };
     int64_t row = (int64_t)blockIdx.x * kTeams + team;
-    if (row < a.rows) fetch(row);
+    if (kAhead && row < a.rows) fetch(row);
     int slot = 0;
     for (; row < a.rows; row += step) {
-        float n[C][8], h[C][8], add[C][8];      // c, then h; g is in `add` till h is there
+        if (!kAhead) fetch(row);
+        float n[C][8], h[C][8], add[C][8];
         const float r = rstd;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -211,9 +213,9 @@ void layer_norm_bwd_kernel(NormBwd a)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) n[c][k] *= by;
             } else {
-                unpack(raw_x[c], n[c]);
+                unpack<RAGGED>(raw_x[c], left[c], a.cols < 8, n[c]);
             }
-            unpack(raw_g[c], h[c]);
+            unpack<RAGGED>(raw_g[c], left[c], a.cols < 8, h[c]);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 n[c][k] = (n[c][k] - mean) * r;
@@ -221,13 +223,15 @@ void layer_norm_bwd_kernel(NormBwd a)
                 db[c][k] += h[c][k];
                 h[c][k] *= w[c][k];
             }
-            if (a.add && a.d_x) unpack(raw_add[c], add[c]);
-            else {
+            if (kAhead) {
+                if (a.add && a.d_x) unpack<RAGGED>(raw_add[c], left[c], a.cols < 8, add[c]);
+                else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) add[c][k] = 0.0f;
+                    for (int k = 0; k < 8; ++k) add[c][k] = 0.0f;
+                }
             }
         }
-        if (row + step < a.rows) fetch(row + step);
+        if (kAhead && row + step < a.rows) fetch(row + step);
         if (!a.d_x) continue;
         float sums[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -243,6 +247,11 @@ void layer_norm_bwd_kernel(NormBwd a)
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             float d[8];
+            if (!kAhead) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) add[c][k] = 0.0f;
+                if (a.add) unpack<RAGGED>(load_raw<RAGGED>((const T *)a.add + row * a.cols + (c * L + lane) * 8, left[c], a.stream, a.cols < 8), left[c], a.cols < 8, add[c]);
+            }
 #pragma unroll
             for (int k = 0; k < 8; ++k) d[k] = __builtin_fmaf(h[c][k] - one - n[c][k] * two, r, add[c][k]);
             store_first<RAGGED>((T *)a.d_x + row * a.cols + (c * L + lane) * 8, left[c], d, a.stream);
@@ -282,8 +291,9 @@ void layer_norm_bwd_kernel(NormBwd a)
 }
 
 constexpr int kForms = 8;
-// lanes of a row, chunks of a lane: up to 128, 256, 512, 1024, 2048, 4096, 8192 and 32768 entries
-constexpr int kLanes[kForms] = {16, 16, 64, 64, 256, 256, 256, 1024}, kChunksOf[kForms] = {1, 2, 1, 2, 1, 2, 4, 4};
+// lanes of a row, chunks of a lane: up to 128, 256, 512, 1024, 2048, 4096, 8192 and 16384 entries (in 1024 lanes, longer rows would spill: 2000 x 16384 backward 520 us so)
+constexpr int kLanes[kForms] = {16, 16, 64, 64, 256, 256, 256, 512}, kChunksOf[kForms] = {1, 2, 1, 2, 1, 2, 4, 4};
+static_assert(kLanes[kForms - 1] * kChunksOf[kForms - 1] * 8 == kNormMostCols, "the longest row");
 int form_of(int32_t cols)
 {
     int f = 0;
@@ -297,10 +307,12 @@ int64_t fwd_blocks(int form, int64_t rows)
     const int64_t blocks = (rows + teams_of(form) - 1) / teams_of(form), most = kLanes[form] > 256 ? 512 : 2048;
     return blocks < most ? blocks : most;
 }
+// Backward: as many rows for every team, on the blocks that a compute unit holds two of, or one where a block has one row at a time and a thread many registers.  More blocks leave more
+// sums to be added up, and rows that do not come out even (65536 x 768 from eight bits: 384 blocks 82.4 us, 512 71.6, 768 73.7, 1024 81.6; 4096 x 8192: 256 blocks 61.2, 512 70.0).
 int64_t bwd_blocks(int form, int64_t rows)
 {
-    const int64_t blocks = (rows + teams_of(form) - 1) / teams_of(form), most = kLanes[form] > 256 ? 256 : 1024;
-    return blocks < most ? blocks : most;
+    const int64_t teams = teams_of(form), most = teams == 1 && kChunksOf[form] > 1 ? 256 : 512, per = (rows + most * teams - 1) / (most * teams);
+    return (rows + per * teams - 1) / (per * teams);
 }
 int64_t part_cols(int32_t cols) { return ((int64_t)cols + 7) / 8 * 8; }
 
@@ -311,7 +323,7 @@ int launch_fwd(const NormFwd &a, hipStream_t stream)
     typedef void (*kernel_t)(NormFwd);
     static const kernel_t kernels[kForms] = {layer_norm_fwd_kernel<T, 16, 1, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 16, 2, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 64, 1, RAGGED, KEEP>,
                                              layer_norm_fwd_kernel<T, 64, 2, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 256, 1, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 256, 2, RAGGED, KEEP>,
-                                             layer_norm_fwd_kernel<T, 256, 4, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 1024, 4, RAGGED, KEEP>};
+                                             layer_norm_fwd_kernel<T, 256, 4, RAGGED, KEEP>, layer_norm_fwd_kernel<T, 512, 4, RAGGED, KEEP>};
     CDL_LAUNCH("layer_norm_fwd_kernel", stream, kernels[form], dim3((unsigned)fwd_blocks(form, a.rows_end)), dim3(kLanes[form] > 256 ? kLanes[form] : 256), 0, a);
     return check_launch();
 }
@@ -329,7 +341,7 @@ int launch_bwd(const NormBwd &a, hipStream_t stream)
     typedef void (*kernel_t)(NormBwd);
     static const kernel_t kernels[kForms] = {layer_norm_bwd_kernel<T, 16, 1, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 16, 2, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 64, 1, RAGGED, KEPT>,
                                              layer_norm_bwd_kernel<T, 64, 2, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 256, 1, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 256, 2, RAGGED, KEPT>,
-                                             layer_norm_bwd_kernel<T, 256, 4, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 1024, 4, RAGGED, KEPT>};
+                                             layer_norm_bwd_kernel<T, 256, 4, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 512, 4, RAGGED, KEPT>};
     CDL_LAUNCH("layer_norm_bwd_kernel", stream, kernels[form], dim3((unsigned)bwd_blocks(form, a.rows)), dim3(kLanes[form] > 256 ? kLanes[form] : 256), 0, a);
     return check_launch();
 }

@@ -45,7 +45,7 @@ def backward(torch, cdl, g, mean, rstd, want="xwb", fmt="e4m3", **given):
 
 # every number of lanes and chunks of a row, whole and ragged, one row to many
 SIZES = [(1, 1), (3, 7), (5, 8), (33, 64), (130, 127), (129, 128), (257, 129), (64, 200), (300, 256), (17, 257), (40, 512), (1000, 513), (7, 768), (4100, 1021), (515, 1024), (9, 1025),
-         (33, 2047), (21, 2048), (6, 3001), (12, 4096), (5, 4097), (4, 8192), (3, 8200), (2, 16384), (3, 20001), (2, 32768), (1, 32767), (2600, 1536), (20000, 40)]
+         (33, 2047), (21, 2048), (6, 3001), (12, 4096), (5, 4097), (4, 8192), (3, 8200), (2, 16384), (3, 15001), (300, 16376), (1, 16383), (2600, 1536), (20000, 40)]
 
 
 @pytest.mark.parametrize("kind", KINDS)

@@ -84,7 +84,7 @@ def test_numbers(cdl, make):
         assert call(eps=-1e-9) == call(eps=float("nan")) == call(eps=float("inf")) == PARAM
     if make in (norm_fwd, norm_bwd):
         assert call(cols=0) == PARAM
-        assert call(cols=32769) == call(rows=(1 << 30) + 1) == call(rows=(1 << 30) - 1, cols=32768) == RANGE
+        assert call(cols=16385) == call(rows=(1 << 30) + 1) == call(rows=(1 << 30) - 1, cols=16384 + 1) == RANGE
     elif "rows" in call.args:
         assert call(cols=(1 << 24) + 1) == call(rows=(1 << 30) + 1) == call(rows=1 << 21, cols=(1 << 23) + 1) == RANGE
     else:
@@ -140,7 +140,7 @@ def test_scratch(cdl):
         assert f(0, 8) == f(-1, 8) == f(8, -1) == f((1 << 30) + 1, 8) == 0
         assert f(1000, 300) > 0 and f(1000, 300) % 256 == 0
         assert f(1 << 20, 300) <= 64 << 20      # not with the rows
-    assert norm(8, 32769) == act(8, (1 << 24) + 1) == 0 and act(1000, 300) < gate(1000, 300) <= 2 * act(1000, 300)
+    assert norm(8, 16385) == act(8, (1 << 24) + 1) == 0 and act(1000, 300) < gate(1000, 300) <= 2 * act(1000, 300)
     for call, need in ((norm_bwd(cdl), norm(8, 8)), (act_bwd(cdl), act(8, 8)), (gated_bwd(cdl), gate(8, 8))):
         assert call(ws_bytes=need - 1) == call(ws=None) == WS and call(ws=FAKE + 128) == ALIGN
     for f, call in ((cdl.block8_gemm_act_workspace_bytes, product(cdl)), (cdl.block8_gemm_gated_workspace_bytes, gated(cdl))):
@@ -263,7 +263,7 @@ def test_largest_sizes(tmp_path, type_):
 
     def act(rows, cols):
         return ("cdl_act_bwd", [(POINTER, A), (INT, type_), (POINTER, A), (POINTER, None), (POINTER, None), (INT, 0), (INT, GELU), (INT, rows), (INT, cols)] + [(POINTER, A)] * 3 + WS_)
-    calls = [norm(rows, cols, back) for rows, cols in ((1 << 30, 128), (1 << 29, 32768), (1, 32768)) for back in (False, True)]
+    calls = [norm(rows, cols, back) for rows, cols in ((1 << 30, 128), (1 << 29, 16384), (1, 16384)) for back in (False, True)]
     calls += [act(1 << 30, 1 << 14), act(1 << 20, 1 << 24), act(1, 1 << 24)]
     calls += [c_product(M, N, K, type_, sides=sides) for sides in (1, 2) for M, N, K in ((1 << 30, 1 << 14, 128), (1 << 14, 1 << 30, 128), (1, 1 << 30, 1 << 20), (1 << 30, 1, 128), (1 << 22, 1 << 22, 0))]
     for call, (launches, _) in zip(calls, launch_recorder.record(tmp_path, calls)):

@@ -261,9 +261,12 @@ void block8_act_kernel(RingCall<ActStore<FORM, T>> call)
     ring<FORM, OpF8<FP, FQ, EXACT>, false, false, false>(call);
 }
 
-// 256 x 256 with one block on a compute unit, 128 x 128 with two: while one finishes a tile, the other multiplies.
+// Tiles of 256 x 256, one block on a compute unit; of 128 x 128, two: while one finishes a tile, the other multiplies; of 64 x 64 (gated: 128 x 64, 64 of either matrix), two, with more
+// K-tiles under way: for products of so few tiles that their latency counts.
 template <bool GATED> using ActWide = RingForm<2, 2, 4, 4, 2, 2, 1, 4096, true, GATED>;
 template <bool GATED> using ActPair = RingForm<2, 2, 2, 2, 2, 2, 2, 2048, true, GATED>;
+template <bool GATED> using ActSmall = std::conditional_t<GATED, RingForm<2, 2, 2, 1, 3, 3, 2, 0, true, true>, RingForm<2, 2, 1, 1, 4, 4, 2, 0, true, false>>;
+enum class ActForm { kWide, kPair, kSmall };
 
 template <class FORM, bool EXACT, class T>
 int launch_act_form(RingJob job, const ActTarget &to, int a_format, int b_format, hipStream_t stream)
@@ -280,17 +283,20 @@ int launch_act_form(RingJob job, const ActTarget &to, int a_format, int b_format
     return check_launch();
 }
 
-// One file for each type of results and number of projections: they take a minute each to compile.
+// One file for each type of results and number of projections: they take a minute or two each to compile.
 template <bool GATED, class T>
-int launch_act_ring(bool wide, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream)
+int launch_act_ring(ActForm form, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream)
 {
     constexpr bool kExact = sizeof(T) == 4;
-    if constexpr (kExact && !GATED) return launch_act_form<ActPair<GATED>, kExact, T>(job, to, a_format, b_format, stream);      // (wide tiles spill: act_cost())
-    else return wide ? launch_act_form<ActWide<GATED>, kExact, T>(job, to, a_format, b_format, stream) : launch_act_form<ActPair<GATED>, kExact, T>(job, to, a_format, b_format, stream);
+    if (form == ActForm::kSmall) return launch_act_form<ActSmall<GATED>, kExact, T>(job, to, a_format, b_format, stream);
+    if constexpr (!kExact || GATED) {      // (exact products in wide tiles spill where a tile has four accumulators a row: ring_us())
+        if (form == ActForm::kWide) return launch_act_form<ActWide<GATED>, kExact, T>(job, to, a_format, b_format, stream);
+    }
+    return launch_act_form<ActPair<GATED>, kExact, T>(job, to, a_format, b_format, stream);
 }
-int launch_act_bf16(bool wide, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream);
-int launch_act_f32(bool wide, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream);
-int launch_gated_bf16(bool wide, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream);
-int launch_gated_f32(bool wide, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream);
+int launch_act_bf16(ActForm form, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream);
+int launch_act_f32(ActForm form, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream);
+int launch_gated_bf16(ActForm form, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream);
+int launch_gated_f32(ActForm form, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream);
 
 }  // namespace cdl

@@ -73,30 +73,33 @@ int launch_finish(const Finish &f, int act, bool gated, hipStream_t stream)
     return gated ? launch_finish<T, true, true>(f, act, stream) : launch_finish<T, false, true>(f, act, stream);
 }
 
-// How a product is formed: in fp32 through memory, its contraction in parts; in tiles of 256 x 256, or of 128 x 128 two to a compute unit, finished from the accumulators;
-// or by blocks of 16 rows of the weights.
-enum Way { kParts, kWide, kPair, kThin };
+// How a product is formed: in fp32 through memory, its contraction in parts; in tiles that are finished from the accumulators; or by blocks of 16 rows of the weights.
+enum Way { kParts, kWide, kPair, kSmall, kThin };
 struct Choice {
     Way way;
     int rows;      // kThin: rows of a, in sixteens
 };
 
-// The way that takes least, in us.  A K-tile of 256 x 256 takes 1.72 us (from fp8 in the exact instructions 3.2), one of 128 x 128 1.0 with another block beside it and 0.7 alone
-// (1.8, 1.2); the epilogue of a tile 7 us and 3.5, with gelu 15 and 4.5: the two blocks of a compute unit share the time that one would wait for the other's.  Thin blocks read their rows from L2 at 8 MB
-// a us, behind the latency of a wave's own K-tiles.  Measured, us, as Parts, Wide, Pair, Thin:
-//   4 x 4096 x 1024 gelu            9.5     -     11.1   5.3         1 x 2048 x 768 gated            15.1     -      8.4    5.8
-//   64 x 4096 x 4096 gelu          16.3     -     26.7  12.7         128 x 4096 x 4096 gelu          16.5     -     27.4   23.6
-//   300 x 400 x 9000 gelu          13.5     -     52.8  15.4         1000 x 4096 x 1024 gelu         23.2   32.4    13.6    -
-//   2048 x 2048 x 2048             23.0   31.9    15.7   -           65536 x 4096 x 768               602    293     336    -
-//   65536 x 4096 x 768 gelu         609    417     370   -           65536 x 2048 x 768 gated, z kept 687    371     392    -
-//   32768 x 4096 x 768 gated, fp32  744    433     459   -           32768 x 4096 x 768, fp32         436  (423)     272    -
-float ring_us(bool wide, bool gated, bool exact, int32_t M, int32_t N, int nk, int act)
+// The way that takes least, in us.  Tiles: rounds of blocks over the chip, of a K-tile for every 128 entries of the contraction and the end of a tile, which a compute unit's other block
+// works beside.  Thin blocks read their rows from L2 at 9 MB a us (exact products 6), behind the latency of a wave's own K-tiles.  Measured, us, as Parts, Wide, Pair, Small, Thin:
+//   4 x 4096 x 1024 gelu             9.5    -   11.1    -    5.3        1 x 2048 x 768 gated             15.1    -    8.4    -    5.8
+//   64 x 4096 x 4096 gelu           16.3    -   26.7    -   12.7        64 x 8192 x 2048 gated           21.4    -   15.8  10.6  17.8
+//   300 x 400 x 9000 gelu           13.5    -   52.8  21.3  15.4        256 x 4096 x 4096                17.1    -   24.8  12.0  45.1
+//   1021 x 1000 x 520 gelu, fp32    13.4    -   15.4   8.5  13.1        512 x 2048 x 768 gated           16.8    -    8.3   7.2  18.0
+//   2048 x 2048 x 2048              23.0  31.9  15.7    -     -         8192 x 2048 x 768 gelu             -     -   26.5  39.4    -
+//   65536 x 4096 x 768               602   293   336    -     -         65536 x 4096 x 768 gelu           609   417   370    -     -
+//   65536 x 2048 x 768 gated, z kept 687   371   392    -     -         32768 x 4096 x 768, fp32          436  (423)  272    -     -
+//   32768 x 4096 x 768 gated, fp32   744   433   459    -     -
+struct Cost { int p, q, places; float alone, full, end, gelu; };      // entries of a tile, blocks at a time; us of a K-tile alone on a compute unit and beside another block; the end of a tile, with gelu more
+float tiles_us(Way way, bool gated, bool exact, int32_t M, int32_t N, int nk, int act)
 {
-    const int p = (wide ? 256 : 128) / (gated ? 2 : 1), q = wide ? 256 : 128, places = wide ? 256 : 512;
-    const int64_t tiles = (((int64_t)N + p - 1) / p) * (((int64_t)M + q - 1) / q), rounds = (tiles + places - 1) / places;
-    const float tile = wide ? (exact ? 3.2f : 1.72f) : tiles <= 256 ? (exact ? 1.2f : 0.7f) : exact ? 1.8f : 1.0f;
-    const float end = wide ? (act == CDL_ACT_GELU ? 15.0f : 7.0f) : act == CDL_ACT_GELU ? 4.5f : 3.5f;
-    return 4.0f + (float)rounds * ((float)nk * tile + end);
+    const Cost c = way == kWide   ? Cost{256, 256, 256, exact ? 3.2f : 1.72f, exact ? 3.2f : 1.72f, 7.0f, 8.0f}
+                   : way == kPair ? Cost{128, 128, 512, exact ? 1.2f : 0.7f, exact ? 1.8f : 1.0f, 3.5f, 1.0f}
+                   : gated        ? Cost{128, 64, 512, exact ? 0.6f : 0.28f, exact ? 1.6f : 0.62f, 1.7f, 0.3f}
+                                  : Cost{64, 64, 512, exact ? 0.5f : 0.23f, exact ? 0.8f : 0.4f, 1.7f, 0.3f};
+    const int p = gated ? c.p / 2 : c.p;
+    const int64_t tiles = (((int64_t)N + p - 1) / p) * (((int64_t)M + c.q - 1) / c.q), rounds = (tiles + c.places - 1) / c.places;
+    return 4.0f + (float)rounds * ((float)nk * (tiles <= 256 ? c.alone : c.full) + c.end + (act == CDL_ACT_GELU ? c.gelu : 0.0f));
 }
 Choice choose(int32_t M, int32_t N, int32_t K, bool gated, int y_type, int act)
 {
@@ -105,18 +108,18 @@ Choice choose(int32_t M, int32_t N, int32_t K, bool gated, int y_type, int act)
     const int nk = (int)(block8_pitch(K) / kRingRow);
     Choice best{kParts, 0};
     float least = block8_parts_us(M, N, K) * (gated ? 2.0f : 1.0f) * (exact ? 1.5f : 1.0f);
-    for (const bool wide : {false, true}) {
-        if (wide && exact && !gated) continue;
-        const float us = ring_us(wide, gated, exact, M, N, nk, act);
+    for (const Way way : {kSmall, kPair, kWide}) {
+        if (way == kWide && exact && !gated) continue;      // (it spills)
+        const float us = tiles_us(way, gated, exact, M, N, nk, act);
         if (us < least) {
             least = us;
-            best.way = wide ? kWide : kPair;
+            best.way = way;
         }
     }
     for (const int rows : {1, 2, 4}) {
         const int64_t across = ((int64_t)M + 16 * rows - 1) / (16 * rows), blocks = ((int64_t)N + 15) / 16 * across;
         const float read = (float)((gated ? 2 : 1) + rows);      // sixteens of a block
-        const float us = 4.0f + (float)blocks * 16.0f * read * (float)block8_pitch(K) / 8e6f + 0.2f * read * (float)((nk + 7) / 8) + 2.0f * (float)(blocks / 512);
+        const float us = 3.5f + (float)blocks * 16.0f * read * (float)block8_pitch(K) / (exact ? 6e6f : 9e6f) + 0.2f * read * (float)((nk + 7) / 8) + (float)(blocks / 512);
         if (us < least && across <= 65535) {
             least = us;
             best = {kThin, rows};
@@ -165,7 +168,8 @@ int launch_block8_gemm_act(const ProductCall &c, bool gated, hipStream_t stream)
         job.pitch_sp = pitch_b;
         job.pitch_sq = pitch_a;
         const auto launch = c.y_type == CDL_BF16 ? (gated ? launch_gated_bf16 : launch_act_bf16) : gated ? launch_gated_f32 : launch_act_f32;
-        return launch(choice.way == kWide, job, to, c.a_format, c.b_format, stream);
+        const ActForm form = choice.way == kWide ? ActForm::kWide : choice.way == kPair ? ActForm::kPair : ActForm::kSmall;
+        return launch(form, job, to, c.a_format, c.b_format, stream);
     }
     Finish f{};
     f.splits = block8_parts(c.M, c.N, c.K);

@@ -3,9 +3,9 @@
 
 namespace cdl {
 
-int launch_act_f32(bool wide, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream)
+int launch_act_f32(ActForm form, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream)
 {
-    return launch_act_ring<false, float>(wide, job, to, a_format, b_format, stream);
+    return launch_act_ring<false, float>(form, job, to, a_format, b_format, stream);
 }
 
 }  // namespace cdl

@@ -3,9 +3,9 @@
 
 namespace cdl {
 
-int launch_gated_bf16(bool wide, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream)
+int launch_gated_bf16(ActForm form, const RingJob &job, const ActTarget &to, int a_format, int b_format, hipStream_t stream)
 {
-    return launch_act_ring<true, bf16_t>(wide, job, to, a_format, b_format, stream);
+    return launch_act_ring<true, bf16_t>(form, job, to, a_format, b_format, stream);
 }
 
 }  // namespace cdl

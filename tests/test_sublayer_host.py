@@ -226,7 +226,8 @@ def way(launches):
     assert len(launches) == 1
     if "thin" in names[0]:
         return "thin"
-    return "wide" if "RingForm<2, 2, 4, 4," in names[0] or "RingFormILi2ELi2ELi4ELi4E" in names[0] else "pair"
+    shapes = {"wide": (2, 2, 4, 4, 2, 2), "pair": (2, 2, 2, 2, 2, 2), "small": (2, 2, 1, 1, 4, 4), "small gated": (2, 2, 2, 1, 3, 3)}
+    return next(w.split()[0] for w, s in shapes.items() if "RingForm<%d, %d, %d, %d, %d, %d," % s in names[0] or "RingFormILi%dELi%dELi%dELi%dELi%dELi%dE" % s in names[0])
 
 
 def test_ways_of_the_products(tmp_path):
@@ -239,8 +240,8 @@ def test_ways_of_the_products(tmp_path):
             seen[sides, y_type] = {way(launches) for launches, _ in recorded}
             for launches, _ in recorded:
                 assert all(l.grid[0] * l.threads < 1 << 32 for l in launches)
-    assert seen[1, BF16] == seen[2, BF16] == seen[2, F32] == {"parts", "thin", "pair", "wide"}
-    assert seen[1, F32] == {"parts", "thin", "pair"}
+    assert seen[1, BF16] == seen[2, BF16] == seen[2, F32] == {"parts", "thin", "small", "pair", "wide"}
+    assert seen[1, F32] == {"parts", "thin", "small", "pair"}
 
 
 def test_scratch_is_asked_for_where_it_is_used(tmp_path, cdl):

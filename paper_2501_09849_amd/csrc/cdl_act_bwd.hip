@@ -18,6 +18,7 @@ struct ActBwd {
     int rows, cols, col_blocks, rows_per;
     void *d[2], *y;
     float *parts;                         // [stretch of rows][1 or 2][part_cols], or null
+    float *sums[2];                       // of one stretch alone: where its sums go at once
     int64_t pitch_c, pitch_r, part_cols;
     bool stream;
 };
@@ -94,7 +95,7 @@ void act_bwd_kernel(ActBwd a)
             if (a.d[s]) store_first<RAGGED>((T *)a.d[s] + at, left, d[s], a.stream);
         if (a.y) store_first<RAGGED>((T *)a.y + at, left, y, a.stream);
     }
-    if (!a.parts) return;
+    if (!a.parts && !a.sums[0] && !a.sums[1]) return;
     __shared__ float all[kGroups][kCols];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
@@ -104,7 +105,8 @@ void act_bwd_kernel(ActBwd a)
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) sum += all[i][threadIdx.x];
-        if (cb * kCols + (int)threadIdx.x < a.cols) a.parts[((int64_t)part * S + s) * a.part_cols + cb * kCols + threadIdx.x] = sum;
+        float *const out = a.parts ? a.parts + ((int64_t)part * S + s) * a.part_cols : a.sums[s];
+        if (out && cb * kCols + (int)threadIdx.x < a.cols) out[cb * kCols + threadIdx.x] = sum;
     }
 }
 
@@ -133,14 +135,14 @@ void column_sums_kernel(const float *__restrict__ parts, int64_t n, int sets, in
 
 int64_t part_cols(int32_t cols) { return ((int64_t)cols + 7) / 8 * 8; }
 
-// Stretches of rows: blocks that fill the chip, of at least 16 rows.
+// Stretches of rows: blocks that fill the chip, of at least 16 rows; up to 32 rows are one, whose sums take no second launch.
 struct Split { int col_blocks, parts, rows_per; };
 Split split_of(int32_t rows, int32_t cols)
 {
     Split s;
     s.col_blocks = (cols + kCols - 1) / kCols;
     int64_t parts = (2048 + s.col_blocks - 1) / s.col_blocks;
-    const int64_t most = ((int64_t)rows + 15) / 16;
+    const int64_t most = rows <= 32 ? 1 : ((int64_t)rows + 15) / 16;
     if (parts > most) parts = most;
     s.rows_per = (int)((rows + parts - 1) / parts);
     s.parts = (rows + s.rows_per - 1) / s.rows_per;
@@ -184,7 +186,7 @@ int launch_column_sums(const float *parts, int64_t n, int32_t cols, int64_t pitc
 
 size_t act_bwd_workspace_bytes(int32_t rows, int32_t cols, bool gated)
 {
-    if (rows == 0 || cols == 0) return 0;
+    if (rows == 0 || cols == 0 || split_of(rows, cols).parts == 1) return 0;
     return align_up((size_t)split_of(rows, cols).parts * (gated ? 2 : 1) * (size_t)part_cols(cols) * sizeof(float), 256);
 }
 
@@ -210,7 +212,8 @@ int launch_act_bwd(const ActCall &c, bool gated, hipStream_t stream)
         a.col_blocks = s.col_blocks;
         a.rows_per = s.rows_per;
         a.y = c.y;
-        a.parts = sums ? (float *)c.ws : nullptr;
+        a.parts = sums && parts > 1 ? (float *)c.ws : nullptr;
+        for (int i = 0; i < 2; ++i) a.sums[i] = parts == 1 ? c.d_bias[i] : nullptr;
         a.pitch_c = block8_pitch(c.cols);
         a.pitch_r = block8_pitch(c.rows);
         a.part_cols = part_cols(c.cols);
@@ -219,7 +222,7 @@ int launch_act_bwd(const ActCall &c, bool gated, hipStream_t stream)
         const int rc = gated ? launch_all<true>(a, c.type, c.act, kept, s, stream) : launch_all<false>(a, c.type, c.act, kept, s, stream);
         if (rc != CDL_OK) return rc;
     }
-    return sums ? launch_column_sums((const float *)c.ws, parts, c.cols, part_cols(c.cols), c.d_bias[0], c.d_bias[1], stream, gated ? 2 : 1) : CDL_OK;
+    return sums && parts != 1 ? launch_column_sums((const float *)c.ws, parts, c.cols, part_cols(c.cols), c.d_bias[0], c.d_bias[1], stream, gated ? 2 : 1) : CDL_OK;
 }
 
 }  // namespace cdl

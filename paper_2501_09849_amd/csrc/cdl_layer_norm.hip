@@ -149,6 +149,7 @@ struct NormBwd {
     float by_cols;
     void *d_x;
     float *parts;                      // [block][2][part_cols]: d_w, d_b of the block's rows; or null
+    float *sums[2];                    // of one block alone: where they go at once
     int64_t pitch_c, pitch_r, part_cols;
     bool stream;
 };
@@ -257,8 +258,8 @@ void layer_norm_bwd_kernel(NormBwd a)
             store_first<RAGGED>((T *)a.d_x + row * a.cols + (c * L + lane) * 8, left[c], d, a.stream);
         }
     }
-    if (!a.parts) return;
-    float *const out = a.parts + (int64_t)blockIdx.x * 2 * a.part_cols;
+    if (!a.parts && !a.sums[0] && !a.sums[1]) return;
+    float *const out[2] = {a.parts ? a.parts + (int64_t)blockIdx.x * 2 * a.part_cols : a.sums[0], a.parts ? a.parts + ((int64_t)blockIdx.x * 2 + 1) * a.part_cols : a.sums[1]};
     if constexpr (kTeams > 1) {      // the teams of a block one after the other
         __shared__ float part[2][L * C * 8];
         for (int t = 0; t < kTeams; ++t) {
@@ -274,18 +275,16 @@ void layer_norm_bwd_kernel(NormBwd a)
             }
             __syncthreads();
         }
-        for (int at = threadIdx.x; at < a.part_cols; at += kThreadsOf<L>) {
-            out[at] = part[0][at];
-            out[a.part_cols + at] = part[1][at];
+        for (int at = threadIdx.x; at < a.cols; at += kThreadsOf<L>) {
+            if (out[0]) out[0][at] = part[0][at];
+            if (out[1]) out[1][at] = part[1][at];
         }
     } else {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = (c * L + lane) * 8;
-            if (col < a.part_cols) {
-                store8(out + col, dw[c], false);
-                store8(out + a.part_cols + col, db[c], false);
-            }
+            if (out[0]) store_first<RAGGED>(out[0] + col, left[c], dw[c], false);
+            if (out[1]) store_first<RAGGED>(out[1] + col, left[c], db[c], false);
         }
     }
 }
@@ -309,8 +308,10 @@ int64_t fwd_blocks(int form, int64_t rows)
 }
 // Backward: as many rows for every team, on the blocks that a compute unit holds two of, or one where a block has one row at a time and a thread many registers.  More blocks leave more
 // sums to be added up, and rows that do not come out even (65536 x 768 from eight bits: 384 blocks 82.4 us, 512 71.6, 768 73.7, 1024 81.6; 4096 x 8192: 256 blocks 61.2, 512 70.0).
+// Few rows are one block's, which has the sums without a second launch (16 x 768: 6.9 us instead of 8.9).
 int64_t bwd_blocks(int form, int64_t rows)
 {
+    if (rows <= 4 * teams_of(form)) return 1;
     const int64_t teams = teams_of(form), most = teams == 1 && kChunksOf[form] > 1 ? 256 : 512, per = (rows + most * teams - 1) / (most * teams);
     return (rows + per * teams - 1) / (per * teams);
 }
@@ -367,24 +368,26 @@ int launch_layer_norm_fwd(const void *x, int32_t type, const float *weight, cons
 
 size_t layer_norm_bwd_workspace_bytes(int32_t rows, int32_t cols)
 {
-    if (rows == 0) return 0;
+    if (rows == 0 || bwd_blocks(form_of(cols), rows) == 1) return 0;
     return align_up((size_t)bwd_blocks(form_of(cols), rows) * 2 * (size_t)part_cols(cols) * sizeof(float), 256);
 }
 
 int launch_layer_norm_bwd(const void *g, int32_t type, const void *x, const uint8_t *q, const uint8_t *scale, int32_t format, const float *weight, const float *mean,
                           const float *rstd, const void *add, int32_t rows, int32_t cols, void *d_x, float *d_weight, float *d_bias, void *ws, hipStream_t stream)
 {
-    float *const parts = d_weight || d_bias ? (float *)ws : nullptr;
+    const int64_t blocks = rows > 0 ? bwd_blocks(form_of(cols), rows) : 0;
+    const bool at_once = blocks == 1;
+    float *const parts = (d_weight || d_bias) && !at_once ? (float *)ws : nullptr;
     const int64_t size = type == CDL_BF16 ? 2 : 4;
     if (rows > 0) {
-        const NormBwd a{g, x, q, scale, weight, mean, rstd, add, rows, cols, 1.0f / (float)cols, d_x, parts, block8_pitch(cols), block8_pitch(rows), part_cols(cols),
+        const NormBwd a{g, x, q, scale, weight, mean, rstd, add, rows, cols, 1.0f / (float)cols, d_x, parts, {at_once ? d_weight : nullptr, at_once ? d_bias : nullptr}, block8_pitch(cols), block8_pitch(rows), part_cols(cols),
                         (int64_t)rows * cols * size >= kStreamFrom * 4};
         const int kept = !q ? 0 : format == CDL_E5M2 ? 2 : 1;
         const int rc = type == CDL_BF16 ? launch_bwd<bf16_t>(a, kept, stream) : launch_bwd<float>(a, kept, stream);
         if (rc != CDL_OK) return rc;
     }
-    if (!d_weight && !d_bias) return CDL_OK;
-    return launch_column_sums(parts, rows > 0 ? bwd_blocks(form_of(cols), rows) : 0, cols, part_cols(cols), d_weight, d_bias, stream);
+    if ((!d_weight && !d_bias) || at_once) return CDL_OK;
+    return launch_column_sums(parts, blocks, cols, part_cols(cols), d_weight, d_bias, stream);
 }
 
 }  // namespace cdl

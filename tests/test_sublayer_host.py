@@ -119,10 +119,10 @@ def test_a_copy_in_eight_bits_is_whole_or_absent(cdl):
         z = "x" if make is norm_bwd else "z"
         assert call(**{z: None}) == call(q=FAKE) == call(scale=FAKE) == call(q=FAKE, scale=FAKE) == NULL      # one of the two
         assert call(**{z: None}, q=FAKE) == call(**{z: None}, scale=FAKE) == NULL
-        assert call(**{z: None}, q=FAKE, scale=FAKE, ws_bytes=0) == WS                                       # (as far as the next refusal)
+        assert call(**{z: None}, q=FAKE, scale=FAKE, rows=1000, ws_bytes=0) == WS                            # (as far as the next refusal)
     call = gated_bwd(cdl)
     kept = dict(z=None, z_up=None, q=FAKE, scale=FAKE, q_up=FAKE, scale_up=FAKE)
-    assert call(**kept, ws_bytes=0) == WS
+    assert call(**kept, rows=1000, ws_bytes=0) == WS
     for k in kept:
         assert call(**dict(kept, **{k: FAKE if kept[k] is None else None})) == NULL
     assert call(z=None, q=FAKE, scale=FAKE) == NULL      # both tensors or both in eight bits
@@ -141,8 +141,10 @@ def test_scratch(cdl):
         assert f(1000, 300) > 0 and f(1000, 300) % 256 == 0
         assert f(1 << 20, 300) <= 64 << 20      # not with the rows
     assert norm(8, 16385) == act(8, (1 << 24) + 1) == 0 and act(1000, 300) < gate(1000, 300) <= 2 * act(1000, 300)
-    for call, need in ((norm_bwd(cdl), norm(8, 8)), (act_bwd(cdl), act(8, 8)), (gated_bwd(cdl), gate(8, 8))):
-        assert call(ws_bytes=need - 1) == call(ws=None) == WS and call(ws=FAKE + 128) == ALIGN
+    assert norm(8, 8) == act(8, 8) == gate(32, 8) == 0      # one block alone
+    for make, f in ((norm_bwd, norm), (act_bwd, act), (gated_bwd, gate)):
+        call, need = make(cdl), f(1000, 8)
+        assert call(rows=1000, ws_bytes=need - 1) == call(rows=1000, ws=None) == WS and call(rows=1000, ws=FAKE + 128) == ALIGN
     for f, call in ((cdl.block8_gemm_act_workspace_bytes, product(cdl)), (cdl.block8_gemm_gated_workspace_bytes, gated(cdl))):
         assert f(0, 5, 5) == f(5, 0, 5) == f(5, 5, 0) == f(-1, 5, 5) == f(5, 5, (1 << 23) + 1) == 0
         assert f(1, 4096, 1024) == f(65536, 4096, 1024) == 0                          # finished in the kernel

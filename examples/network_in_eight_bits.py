@@ -1,5 +1,5 @@
-"""A small network trained in eight bits: two layers whose products run on 8-bit floating point, dropout onto a residual, and the cross entropy of a
-linear last layer over a vocabulary, with every gradient.  Synthetic data, plain gradient descent:
+"""A small network trained in eight bits: two layers whose products run on 8-bit floating point, the first one's activation finished with its product, dropout onto a residual, and the
+cross entropy of a linear last layer over a vocabulary, with every gradient.  Synthetic data, plain gradient descent:
 
     python examples/network_in_eight_bits.py [steps]
 
@@ -37,15 +37,16 @@ class Layer:
     def __init__(self, tokens, out, into):
         self.M, self.N, self.K = tokens, out, into
         self.w, self.d_w = torch.randn(out, into, device="cuda") * into ** -0.5, empty(out, into, dtype=torch.float32)
-        self.y, self.d_x = empty(tokens, out, dtype=torch.bfloat16), empty(tokens, into, dtype=torch.bfloat16)
+        self.y, self.z, self.d_x = (empty(tokens, n, dtype=torch.bfloat16) for n in (out, out, into))
         self.x8, self.w8, self.g8 = Blocks(tokens, into), Blocks(out, into, tiles=True), Blocks(tokens, out, format=cdl.E5M2)
-        sizes = ((tokens, out, into), (tokens, into, out), (out, into, tokens))
-        self.ws = empty(max(256, *(cdl.block8_gemm_workspace_bytes(*s) for s in sizes)))
+        sizes = ((tokens, into, out), (out, into, tokens))
+        self.ws = empty(max(256, cdl.block8_gemm_act_workspace_bytes(tokens, out, into), *(cdl.block8_gemm_workspace_bytes(*s) for s in sizes)))
 
-    def forward(self, x):
+    def forward(self, x, act=cdl.ACT_NONE):
+        """act(x w^T), and what the activation is of for its backward pass"""
         self.x8.set(x)
         self.w8.set(self.w)
-        cdl.cdl_block8_gemm(self.x8.q, self.x8.scale, self.w8.q, self.w8.scale, self.M, self.N, self.K, self.y, self.ws)
+        cdl.cdl_block8_gemm_act(self.x8.q, self.x8.scale, self.w8.q, self.w8.scale, self.M, self.N, self.K, self.y, z=None if act == cdl.ACT_NONE else self.z, act=act, ws=self.ws)
         return self.y
 
     def backward(self, g):
@@ -63,7 +64,7 @@ class Network:
         self.up, self.down = Layer(tokens, hidden, width), Layer(tokens, width, hidden)
         self.E = (torch.randn(vocabulary, width, device="cuda") * width ** -0.5).bfloat16()
         self.d_E = torch.empty_like(self.E)
-        self.a, self.d_u = (empty(tokens, hidden, dtype=torch.bfloat16) for _ in range(2))
+        self.d_u = empty(tokens, hidden, dtype=torch.bfloat16)
         self.h, self.d_h, self.d_v = (empty(tokens, width, dtype=torch.bfloat16) for _ in range(3))
         self.loss, self.lse = (empty(tokens, dtype=torch.float32) for _ in range(2))
         self.d_loss = torch.full((tokens,), 1.0 / tokens, device="cuda")
@@ -72,15 +73,13 @@ class Network:
     def step(self, x, target, number):
         """Losses of the tokens, and every gradient."""
         T, D, V = self.T, self.D, self.V
-        u = self.up.forward(x)
-        torch.clamp(u, min=0, out=self.a)
-        v = self.down.forward(self.a)
+        v = self.down.forward(self.up.forward(x, cdl.ACT_RELU))
         counter = number * ((T * D + 7) // 8)                 # no two steps share a part of the sequence
         cdl.cdl_dropout(v, T * D, self.p, self.seed, counter, self.h, add=x)
         cdl.cdl_head_loss_fwd(self.h, self.E, target, T, V, D, self.loss, self.lse, self.ws)
         cdl.cdl_head_loss_bwd(self.h, self.E, target, self.lse, T, V, D, self.d_h, self.d_E, self.ws, d_loss=self.d_loss)
         cdl.cdl_dropout(self.d_h, T * D, self.p, self.seed, counter, self.d_v)
-        torch.mul(self.down.backward(self.d_v), u > 0, out=self.d_u)
+        cdl.cdl_act_bwd(self.down.backward(self.d_v), T, self.up.N, cdl.ACT_RELU, d_z=self.d_u, z=self.up.z)
         self.up.backward(self.d_u)
         return self.loss
 

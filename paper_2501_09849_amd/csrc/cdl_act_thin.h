@@ -8,7 +8,8 @@ namespace cdl {
 // A block: 16 rows of the weights (of both matrices, if GATED) and 16 QT rows of a, its eight waves every eighth K-tile each; their sums meet in LDS.  Nothing
 // is staged and no wave waits for another before that: a lane loads 32 bytes of its row of a K-tile, 16 of either half, and which bytes of a K-tile go to which place of the
 // contraction does not matter as long as both operands agree.
-// Bound by latency for small layers, and by memory for large ones.
+// Bound by latency for small layers (4 x 4096 x 1024 5.3 us a call, 3.7 of them the kernel) and by the way of the weights for large ones (16 x 4096 x 4096 7.6 us for 17 MB).  In
+// tiles of 128 x 64 through LDS the first took 7.4 us for the product alone.
 typedef float v4f __attribute__((ext_vector_type(4)));
 struct ThinJob {
     const uint8_t *a, *b[2], *sa, *sb[2];

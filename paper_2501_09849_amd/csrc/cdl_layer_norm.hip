@@ -3,7 +3,11 @@
 //   m = mean of the row, r = 1 / sqrt(mean of (x - m)^2 + eps), c = (x - m) r;     y = c w + b
 //   h = g w:   d_x = r (h - mean of h - c mean of (h c)) + add,     d_w = sum over rows of g c,     d_b = sum over rows of g
 //
-// A row stays in the registers of L lanes, C chunks of eight entries each, so that it is read once: the mean, then the squares about it, then the results.
+// A row stays in the registers of L lanes, C chunks of eight entries each, so that it is read once: the mean, then the squares about it (a sum of squares less the mean's square would
+// lose rows far from zero), then the results.  Lanes that are not a whole block are a wave or a quarter of one, and their sums never leave the registers.  Weights, and backward the sums over the rows, stay
+// in registers too, so a team takes row after row, the next one's loads under way.
+// Bound by memory, 65536 x 768 in bf16: forward with the copy in eight bits 53 us (252 MB, 4.7 TB/s where a copy reaches 5.2), without 40; backward from eight bits onto a residual 70 us
+// (353 MB, 5.0 TB/s), from bf16 77, and 4 us for adding up the blocks' sums in a launch of their own.  2000 x 16384: forward 28 us, backward 77.
 #include "cdl_block8.h"
 #include "cdl_chunks.h"
 

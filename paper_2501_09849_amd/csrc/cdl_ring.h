@@ -1,5 +1,5 @@
 // Products of two matrices over their contiguous dimension on the matrix cores, bf16 or 8-bit floating point: the loop over
-// K-tiles that the block-scaled product and the loss of the last layer share.
+// K-tiles that the block-scaled product, its forms for layers and the loss of the last layer share.
 //
 //   D[p,q] = sum_k P[p,k] * Q[q,k]
 //

@@ -3,8 +3,8 @@
 // In a GATED form a wave's first half of accumulators along P is of the gate and the second of the same entries of the other projection, so that the product of the two needs no other wave.
 // What it costs: a wave of 128 x 128 is alone on its SIMD and issues the end of a tile in 7500 cycles, with silu in 12700, with gelu in 28600, where six K-tiles take 24500; its stores, one
 // behind the other with those of every other compute unit, take as long as memory takes (128 KB a tile and compute unit in 4.7 us at the 7.2 TB/s that all stores together reach in the caches), and
-// the loads of the next tile come in order behind them.  65536 x 4096 x 768 into bf16: 170 us products and loads alone, 276 with the stores, gelu 417 (in tiles of 128 x 128, where the other block
-// multiplies meanwhile, 370).  65536 x 2048 x 768 gated, all three results kept: 314 us, 805 MB written.
+// the loads of the next tile come in order behind them.  65536 x 4096 x 768 into bf16: 170 us products and loads alone, 270 with the stores, gelu 392 (in tiles of 128 x 128, where the other block
+// multiplies meanwhile, 363).  65536 x 2048 x 768 gated, all three results kept: 313 us, 805 MB written.
 #pragma once
 
 #include "cdl_act.h"
@@ -171,7 +171,7 @@ struct ActStore {
     }
 
     // kSide tiles of an output one behind the other: the halves of a cache line meet in L2.  (With other outputs' between them 17 % more was written than there is, and 65536 x 2048 x 768
-    // gated, all three results kept, took 371 us instead of 314.)
+    // gated, all three results kept, took 371 us instead of 313.)
     static constexpr int kSide = sizeof(T) == 2 && TPO % 2 == 0 ? 2 : 1;
     template <bool FULL>
     __device__ __forceinline__ void store_side_by_side(T *into, int p, int q, int lane, const any_t (&in)[kSide][kCount]) const

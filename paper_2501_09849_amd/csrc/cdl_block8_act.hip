@@ -86,22 +86,23 @@ struct Choice {
 //   64 x 4096 x 4096 gelu           16.3    -   26.7    -   12.7        64 x 8192 x 2048 gated           21.4    -   15.8  10.6  17.8
 //   300 x 400 x 9000 gelu           13.5    -   52.8  21.3  15.4        256 x 4096 x 4096                17.1    -   24.8  12.0  45.1
 //   1021 x 1000 x 520 gelu, fp32    13.4    -   15.4   8.5  13.1        512 x 2048 x 768 gated           16.8    -    8.3   7.2  18.0
-//   2048 x 2048 x 2048              23.0  31.9  15.7    -     -         8192 x 2048 x 768 gelu             -     -   26.5  39.4    -
-//   65536 x 4096 x 768               602   293   336    -     -         65536 x 4096 x 768 gelu           609   417   370    -     -
-//   65536 x 2048 x 768 gated, z kept 687   371   392    -     -         32768 x 4096 x 768, fp32          436  (423)  272    -     -
-//   32768 x 4096 x 768 gated, fp32   744   433   459    -     -
-struct Cost { int p, q, places; float alone, full, end, gelu; };      // entries of a tile, blocks at a time; us of a K-tile alone on a compute unit and beside another block; the end of a tile, with gelu more
-float tiles_us(Way way, bool gated, bool exact, int32_t M, int32_t N, int nk, int act)
+//   2048 x 2048 x 2048              23.0  31.7  16.4    -     -         8192 x 2048 x 768 gelu             -   28.1  25.6  39.4    -
+//   65536 x 4096 x 768               602   270   308    -     -         65536 x 4096 x 768 gelu           609   392   363    -     -
+//   65536 x 2048 x 768 gated         603   255   274    -     -         ... with gelu                       -   302   298    -     -
+//   ... and both z kept              687   313   374    -     -         32768 x 4096 x 768 gated, fp32    744   384   434    -     -
+//   32768 x 4096 x 768, fp32         436  (423)  272    -     -         4096 x 4096 x 4096                 85  57.8  67.8    -     -
+struct Cost { int p, q, places; float alone, full, end, gelu, kept; };      // entries of a tile, blocks at a time; us of a K-tile alone on a compute unit and beside another block; the end of a tile, with gelu and with z kept more
+float tiles_us(Way way, bool gated, bool exact, int32_t M, int32_t N, int nk, int act, bool kept)
 {
-    const Cost c = way == kWide   ? Cost{256, 256, 256, exact ? 3.2f : 1.72f, exact ? 3.2f : 1.72f, 7.0f, 8.0f}
-                   : way == kPair ? Cost{128, 128, 512, exact ? 1.2f : 0.7f, exact ? 1.8f : 1.0f, 3.5f, 1.0f}
-                   : gated        ? Cost{128, 64, 512, exact ? 0.6f : 0.28f, exact ? 1.6f : 0.62f, 1.7f, 0.3f}
-                                  : Cost{64, 64, 512, exact ? 0.5f : 0.23f, exact ? 0.8f : 0.4f, 1.7f, 0.3f};
+    const Cost c = way == kWide   ? Cost{256, 256, 256, exact ? 3.2f : 1.72f, exact ? 3.2f : 1.72f, gated ? 5.3f : 6.3f, gated ? 3.0f : 7.7f, 3.0f}
+                   : way == kPair ? Cost{128, 128, 512, exact ? 1.2f : 0.7f, exact ? 1.8f : 1.0f, gated ? 2.5f : 3.5f, gated ? 0.8f : 1.7f, 3.0f}
+                   : gated        ? Cost{128, 64, 512, exact ? 0.6f : 0.28f, exact ? 1.6f : 0.62f, 1.7f, 0.3f, 0.7f}
+                                  : Cost{64, 64, 512, exact ? 0.5f : 0.23f, exact ? 0.8f : 0.4f, 1.7f, 0.3f, 0.7f};
     const int p = gated ? c.p / 2 : c.p;
     const int64_t tiles = (((int64_t)N + p - 1) / p) * (((int64_t)M + c.q - 1) / c.q), rounds = (tiles + c.places - 1) / c.places;
-    return 4.0f + (float)rounds * ((float)nk * (tiles <= 256 ? c.alone : c.full) + c.end + (act == CDL_ACT_GELU ? c.gelu : 0.0f));
+    return 4.0f + (float)rounds * ((float)nk * (tiles <= 256 ? c.alone : c.full) + c.end + (act == CDL_ACT_GELU ? c.gelu : 0.0f) + (kept ? c.kept : 0.0f));
 }
-Choice choose(int32_t M, int32_t N, int32_t K, bool gated, int y_type, int act)
+Choice choose(int32_t M, int32_t N, int32_t K, bool gated, int y_type, int act, bool kept)
 {
     if (K == 0) return {kParts, 0};
     const bool exact = y_type == CDL_F32;
@@ -110,7 +111,7 @@ Choice choose(int32_t M, int32_t N, int32_t K, bool gated, int y_type, int act)
     float least = block8_parts_us(M, N, K) * (gated ? 2.0f : 1.0f) * (exact ? 1.5f : 1.0f);
     for (const Way way : {kSmall, kPair, kWide}) {
         if (way == kWide && exact && !gated) continue;      // (it spills)
-        const float us = tiles_us(way, gated, exact, M, N, nk, act);
+        const float us = tiles_us(way, gated, exact, M, N, nk, act, kept);
         if (us < least) {
             least = us;
             best.way = way;
@@ -135,10 +136,11 @@ size_t parts_bytes(int32_t M, int32_t N, int32_t K) { return align_up((size_t)bl
 size_t block8_gemm_act_workspace_bytes(int32_t M, int32_t N, int32_t K, bool gated)
 {
     if (M == 0 || N == 0 || K == 0) return 0;
-    // (whatever the results' type and the activation, which the query does not know)
+    // (whatever the results' type, the activation and what is kept, which the query does not know)
     for (const int type : {CDL_BF16, CDL_F32})
         for (const int act : {CDL_ACT_NONE, CDL_ACT_GELU})
-            if (choose(M, N, K, gated, type, act).way == kParts) return parts_bytes(M, N, K) * (gated ? 2 : 1);
+            for (const bool kept : {false, true})
+                if (choose(M, N, K, gated, type, act, kept).way == kParts) return parts_bytes(M, N, K) * (gated ? 2 : 1);
     return 0;
 }
 
@@ -148,7 +150,7 @@ int launch_block8_gemm_act(const ProductCall &c, bool gated, hipStream_t stream)
     const ActTarget to{{c.bias[0], c.bias[1]}, c.add, c.y, {c.z[0], c.z[1]}, c.M, c.N, c.act};
     const int64_t ld = block8_pitch(c.K), pitch_a = block8_pitch(c.M), pitch_b = block8_pitch(c.N);
     const int nk = (int)(ld / kRingRow);
-    const Choice choice = choose(c.M, c.N, c.K, gated, c.y_type, c.act);
+    const Choice choice = choose(c.M, c.N, c.K, gated, c.y_type, c.act, c.z[0] || c.z[1]);
     if (choice.way == kThin)
         return launch_thin_any({c.a, {c.b[0], c.b[1]}, c.a_scale, {c.b_scale[0], c.b_scale[1]}, ld, pitch_a, pitch_b, nk, to}, choice.rows, gated, c.y_type, c.a_format, c.b_format,
                                stream);

@@ -30,7 +30,7 @@ HIPCC_FLAGS = [
 
 
 # the ones that take longest to compile, whatever their size: many forms of one loop
-LONG_COMPILES = ("cdl_block8_gemm.hip", "cdl_head_loss.hip")
+LONG_COMPILES = ("cdl_block8_gemm.hip", "cdl_head_loss.hip", "cdl_block8_act_bf16.hip", "cdl_block8_act_f32.hip", "cdl_block8_gated_bf16.hip", "cdl_block8_gated_f32.hip")
 
 
 def sources():

@@ -113,11 +113,11 @@ void act_bwd_kernel(ActBwd a)
     }
 }
 
-// Sums of the blocks' parts [parts][sets][pitch] over the first index, in order: 16 columns a block, 64 threads each.
+// Sums of the blocks' parts [parts][sets][pitch] over the first index: 16 columns a block, 64 threads each, whose sums are joined in a fixed order.
 __global__ __launch_bounds__(1024)
 void column_sums_kernel(const float *__restrict__ parts, int64_t n, int sets, int64_t cols, int64_t pitch, float *out0, float *out1)
 {
-    __shared__ float all[64][16];
+    __shared__ float all[16][16];
     const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
     const int64_t col = (int64_t)blockIdx.x * 16 + lane;
     float *const out = blockIdx.y ? out1 : out0;
@@ -127,11 +127,14 @@ void column_sums_kernel(const float *__restrict__ parts, int64_t n, int sets, in
 #pragma unroll 8
         for (int64_t i = group; i < n; i += 64) sum += parts[(i * sets + blockIdx.y) * pitch + col];
     }
-    all[group][lane] = sum;
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if ((threadIdx.x & 63) < 16) all[threadIdx.x >> 6][lane] = sum;
     __syncthreads();
     if (threadIdx.x < 16 && col < cols) {
         sum = 0.0f;
-        for (int i = 0; i < 64; ++i) sum += all[i][lane];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += all[i][lane];
         out[col] = sum;
     }
 }

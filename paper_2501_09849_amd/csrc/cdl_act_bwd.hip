@@ -12,8 +12,15 @@
 namespace cdl {
 namespace {
 
-// A block: 256 columns, 32 lanes of eight each, eight rows at a time of its stretch of rows; a thread's sums of its columns stay in registers.
-constexpr int kLanes = 32, kGroups = 8, kThreads = kLanes * kGroups, kCols = kLanes * 8;
+// A block: 256 columns, 32 lanes of eight each, eight rows at a time of its stretch of rows; a thread's sums of its columns stay in registers.  TALL: 64 columns, 64 rows at a
+// time, for sums of few rows, which one block then has whole: a second launch that adds up parts takes about
+// 3.5 us (74 x 75 in fp32 8.5 us with it, 5.0 without; 384 x 576 in bf16 from eight bits 8.9 and 5.3).  From 385 rows on the longer walk costs what the launch did: gelu, 385 x 2048 in bf16, 7.9 us
+// in two launches, 384 rows 7.5 in one; 512 rows 7.9 and 9.0.
+template <bool TALL> constexpr int kLanes = TALL ? 8 : 32;
+template <bool TALL> constexpr int kGroups = TALL ? 64 : 8;
+template <bool TALL> constexpr int kThreads = kLanes<TALL> * kGroups<TALL>;
+template <bool TALL> constexpr int kCols = kLanes<TALL> * 8;
+constexpr int kTallRows = 384;
 
 struct ActBwd {
     const void *g, *z[2];                 // z of the gate (or of the layer), and of the other projection
@@ -26,14 +33,14 @@ struct ActBwd {
     bool stream;
 };
 
-template <class T, int ACT, bool GATED, bool RAGGED, int KEPT>      // KEPT: 0 no, 1 E4M3, 2 E5M2
-__global__ __launch_bounds__(kThreads)
+template <class T, int ACT, bool GATED, bool RAGGED, int KEPT, bool TALL>      // KEPT: 0 no, 1 E4M3, 2 E5M2
+__global__ __launch_bounds__(kThreads<TALL>)
 void act_bwd_kernel(ActBwd a)
 {
-    constexpr int S = GATED ? 2 : 1;
-    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+    constexpr int S = GATED ? 2 : 1, kRows = kGroups<TALL>, kAcross = kCols<TALL>;
+    const int lane = threadIdx.x % kLanes<TALL>, group = threadIdx.x / kLanes<TALL>;
     const int cb = (int)(blockIdx.x % (unsigned)a.col_blocks), part = (int)(blockIdx.x / (unsigned)a.col_blocks);
-    const int col = cb * kCols + lane * 8, left = a.cols - col;
+    const int col = cb * kAcross + lane * 8, left = a.cols - col;
     const int64_t first = (int64_t)part * a.rows_per, end = min(first + a.rows_per, (int64_t)a.rows);
     Raw8<T> raw_g, raw_z[S];
     u32x2 kept[S];
@@ -63,7 +70,7 @@ void act_bwd_kernel(ActBwd a)
         for (int k = 0; k < 8; ++k) sums[s][k] = 0.0f;
     int64_t row = first + group;
     if (row < end) fetch(row);
-    for (; row < end; row += kGroups) {
+    for (; row < end; row += kRows) {
         float g[8], z[S][8], d[S][8], y[8];
         unpack<RAGGED>(raw_g, left, a.cols < 8, g);
 #pragma unroll
@@ -77,7 +84,7 @@ void act_bwd_kernel(ActBwd a)
                 unpack<RAGGED>(raw_z[s], left, a.cols < 8, z[s]);
             }
         }
-        if (row + kGroups < end) fetch(row + kGroups);
+        if (row + kRows < end) fetch(row + kRows);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const ValueSlope v = act_both<ACT>(z[0][k]);
@@ -99,17 +106,19 @@ void act_bwd_kernel(ActBwd a)
         if (a.y) store_first<RAGGED>((T *)a.y + at, left, y, a.stream);
     }
     if (!a.parts && !a.sums[0] && !a.sums[1]) return;
-    __shared__ float all[kGroups][kCols];
+    __shared__ float all[kRows][kAcross];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
         if (s > 0) __syncthreads();
         store8(&all[group][lane * 8], sums[s], false);
         __syncthreads();
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) sum += all[i][threadIdx.x];
         float *const out = a.parts ? a.parts + ((int64_t)part * S + s) * a.part_cols : a.sums[s];
-        if (out && cb * kCols + (int)threadIdx.x < a.cols) out[cb * kCols + threadIdx.x] = sum;
+        if (out && threadIdx.x < kAcross && cb * kAcross + (int)threadIdx.x < a.cols) {
+            float sum = 0.0f;
+#pragma unroll 8
+            for (int i = 0; i < kRows; ++i) sum += all[i][threadIdx.x];
+            out[cb * kAcross + threadIdx.x] = sum;
+        }
     }
 }
 
@@ -141,12 +150,22 @@ void column_sums_kernel(const float *__restrict__ parts, int64_t n, int sets, in
 
 int64_t part_cols(int32_t cols) { return ((int64_t)cols + 7) / 8 * 8; }
 
-// Stretches of rows: blocks that fill the chip, of at least 16 rows; up to 32 rows are one, whose sums take no second launch.
-struct Split { int col_blocks, parts, rows_per; };
-Split split_of(int32_t rows, int32_t cols)
+// Stretches of rows: blocks that fill the chip, of at least 16 rows; up to 32 rows, and where sums are asked for up to 384, are one, whose sums take no second launch.
+struct Split {
+    int col_blocks, parts, rows_per;
+    bool tall;
+};
+Split split_of(int32_t rows, int32_t cols, bool sums)
 {
     Split s;
-    s.col_blocks = (cols + kCols - 1) / kCols;
+    s.tall = sums && rows > 32 && rows <= kTallRows;
+    if (s.tall) {
+        s.col_blocks = (cols + kCols<true> - 1) / kCols<true>;
+        s.parts = 1;
+        s.rows_per = rows;
+        return s;
+    }
+    s.col_blocks = (cols + kCols<false> - 1) / kCols<false>;
     int64_t parts = (2048 + s.col_blocks - 1) / s.col_blocks;
     const int64_t most = rows <= 32 ? 1 : ((int64_t)rows + 15) / 16;
     if (parts > most) parts = most;
@@ -155,30 +174,37 @@ Split split_of(int32_t rows, int32_t cols)
     return s;
 }
 
-template <class T, int ACT, bool GATED, bool RAGGED>
+template <class T, int ACT, bool GATED, bool RAGGED, bool TALL>
 int launch_act(const ActBwd &a, int kept, int64_t blocks, hipStream_t stream)
 {
-    const auto kernel = kept == 0 ? act_bwd_kernel<T, ACT, GATED, RAGGED, 0> : kept == 1 ? act_bwd_kernel<T, ACT, GATED, RAGGED, 1> : act_bwd_kernel<T, ACT, GATED, RAGGED, 2>;
-    CDL_LAUNCH(GATED ? "gated_bwd_kernel" : "act_bwd_kernel", stream, kernel, dim3((unsigned)blocks), dim3(kThreads), 0, a);
+    const auto kernel = kept == 0   ? act_bwd_kernel<T, ACT, GATED, RAGGED, 0, TALL>
+                        : kept == 1 ? act_bwd_kernel<T, ACT, GATED, RAGGED, 1, TALL>
+                                    : act_bwd_kernel<T, ACT, GATED, RAGGED, 2, TALL>;
+    CDL_LAUNCH(GATED ? "gated_bwd_kernel" : "act_bwd_kernel", stream, kernel, dim3((unsigned)blocks), dim3(kThreads<TALL>), 0, a);
     return check_launch();
 }
+template <class T, int ACT, bool GATED, bool RAGGED>
+int launch_act(const ActBwd &a, int kept, const Split &s, hipStream_t stream)
+{
+    const int64_t blocks = (int64_t)s.col_blocks * s.parts;
+    return s.tall ? launch_act<T, ACT, GATED, RAGGED, true>(a, kept, blocks, stream) : launch_act<T, ACT, GATED, RAGGED, false>(a, kept, blocks, stream);
+}
 template <class T, bool GATED, bool RAGGED>
-int launch_any(const ActBwd &a, int act, int kept, int64_t blocks, hipStream_t stream)
+int launch_any(const ActBwd &a, int act, int kept, const Split &s, hipStream_t stream)
 {
     switch (act) {
-        case CDL_ACT_RELU: return launch_act<T, CDL_ACT_RELU, GATED, RAGGED>(a, kept, blocks, stream);
-        case CDL_ACT_GELU: return launch_act<T, CDL_ACT_GELU, GATED, RAGGED>(a, kept, blocks, stream);
-        case CDL_ACT_SILU: return launch_act<T, CDL_ACT_SILU, GATED, RAGGED>(a, kept, blocks, stream);
-        default: return launch_act<T, CDL_ACT_NONE, GATED, RAGGED>(a, kept, blocks, stream);
+        case CDL_ACT_RELU: return launch_act<T, CDL_ACT_RELU, GATED, RAGGED>(a, kept, s, stream);
+        case CDL_ACT_GELU: return launch_act<T, CDL_ACT_GELU, GATED, RAGGED>(a, kept, s, stream);
+        case CDL_ACT_SILU: return launch_act<T, CDL_ACT_SILU, GATED, RAGGED>(a, kept, s, stream);
+        default: return launch_act<T, CDL_ACT_NONE, GATED, RAGGED>(a, kept, s, stream);
     }
 }
 template <bool GATED>
 int launch_all(ActBwd a, int type, int act, int kept, const Split &s, hipStream_t stream)
 {
-    const int64_t blocks = (int64_t)s.col_blocks * s.parts;
     if (a.cols % 8 == 0)
-        return type == CDL_BF16 ? launch_any<bf16_t, GATED, false>(a, act, kept, blocks, stream) : launch_any<float, GATED, false>(a, act, kept, blocks, stream);
-    return type == CDL_BF16 ? launch_any<bf16_t, GATED, true>(a, act, kept, blocks, stream) : launch_any<float, GATED, true>(a, act, kept, blocks, stream);
+        return type == CDL_BF16 ? launch_any<bf16_t, GATED, false>(a, act, kept, s, stream) : launch_any<float, GATED, false>(a, act, kept, s, stream);
+    return type == CDL_BF16 ? launch_any<bf16_t, GATED, true>(a, act, kept, s, stream) : launch_any<float, GATED, true>(a, act, kept, s, stream);
 }
 
 }  // namespace
@@ -192,8 +218,8 @@ int launch_column_sums(const float *parts, int64_t n, int32_t cols, int64_t pitc
 
 size_t act_bwd_workspace_bytes(int32_t rows, int32_t cols, bool gated)
 {
-    if (rows == 0 || cols == 0 || split_of(rows, cols).parts == 1) return 0;
-    return align_up((size_t)split_of(rows, cols).parts * (gated ? 2 : 1) * (size_t)part_cols(cols) * sizeof(float), 256);
+    if (rows == 0 || cols == 0 || split_of(rows, cols, true).parts == 1) return 0;
+    return align_up((size_t)split_of(rows, cols, true).parts * (gated ? 2 : 1) * (size_t)part_cols(cols) * sizeof(float), 256);
 }
 
 int launch_act_bwd(const ActCall &c, bool gated, hipStream_t stream)
@@ -203,7 +229,7 @@ int launch_act_bwd(const ActCall &c, bool gated, hipStream_t stream)
     const int64_t size = c.type == CDL_BF16 ? 2 : 4;
     int64_t parts = 0;
     if (c.rows > 0) {
-        const Split s = split_of(c.rows, c.cols);
+        const Split s = split_of(c.rows, c.cols, sums);
         parts = s.parts;
         ActBwd a{};
         a.g = c.g;

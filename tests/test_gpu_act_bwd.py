@@ -8,7 +8,7 @@ import sublayer_util as su
 
 pytestmark = pytest.mark.gpu
 KINDS = ("float32", "bfloat16")
-SIZES = [(1, 1), (1, 1000), (2, 7), (5, 8), (16, 256), (17, 257), (100, 130), (333, 1000), (1000, 2049), (4099, 520), (20000, 24), (3, 70001)]
+SIZES = [(1, 1), (1, 1000), (2, 7), (5, 8), (16, 256), (17, 257), (100, 130), (333, 1000), (1000, 2049), (4099, 520), (20000, 24), (3, 70001), (33, 64), (97, 7), (384, 200), (385, 65)]
 
 
 @pytest.fixture(scope="module")

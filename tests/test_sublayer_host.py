@@ -141,7 +141,7 @@ def test_scratch(cdl):
         assert f(1000, 300) > 0 and f(1000, 300) % 256 == 0
         assert f(1 << 20, 300) <= 64 << 20      # not with the rows
     assert norm(8, 16385) == act(8, (1 << 24) + 1) == 0 and act(1000, 300) < gate(1000, 300) <= 2 * act(1000, 300)
-    assert norm(8, 8) == act(8, 8) == gate(32, 8) == 0      # one block alone
+    assert norm(8, 8) == act(8, 8) == gate(384, 8) == 0      # one block alone
     for make, f in ((norm_bwd, norm), (act_bwd, act), (gated_bwd, gate)):
         call, need = make(cdl), f(1000, 8)
         assert call(rows=1000, ws_bytes=need - 1) == call(rows=1000, ws=None) == WS and call(rows=1000, ws=FAKE + 128) == ALIGN

@@ -513,7 +513,7 @@ enum { CDL_ACT_NONE = 0, CDL_ACT_RELU = 1, CDL_ACT_GELU = 2, CDL_ACT_SILU = 3 };
  *   z[m,n] = (the product of cdl_block8_gemm)[m,n] + bias[n],       y[m,n] = act(z[m,n]) + add[m,n]
  *   bias  fp32[N], nullable;   add  [M,N], nullable (a residual);   y [M,N] required;   z [M,N] nullable, for the backward pass
  * y, add and z are of y_type, which decides on the product's instructions as it does there; z is formed in fp32 and rounded where it is stored, y is of the
- * unrounded one.  y may be add.  K == 0: the product is 0.  Errors and limits as for cdl_block8_gemm, and CDL_ERR_PARAM for an unknown activation.
+ * unrounded one, and the same bits whether z is asked for or not.  y may be add.  K == 0: the product is 0.  Errors and limits as for cdl_block8_gemm, and CDL_ERR_PARAM for an unknown activation.
  * Scratch: cdl_block8_gemm_act_workspace_bytes.
  */
 size_t cdl_block8_gemm_act_workspace_bytes(int32_t M, int32_t N, int32_t K);

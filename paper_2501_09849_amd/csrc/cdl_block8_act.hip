@@ -1,6 +1,8 @@
 // The block-scaled product with what stands behind it in a layer, and the gated product of two projections:
 //
 //   z = a b^T + bias,  y = act(z) + add                    y = act(a gate^T + bias) * (a up^T + bias)
+#include <cmath>
+
 #include "cdl_act_thin.h"
 #include "cdl_chunks.h"
 
@@ -102,21 +104,29 @@ float tiles_us(Way way, bool gated, bool exact, int32_t M, int32_t N, int nk, in
     const int64_t tiles = (((int64_t)N + p - 1) / p) * (((int64_t)M + c.q - 1) / c.q), rounds = (tiles + c.places - 1) / c.places;
     return 4.0f + (float)rounds * ((float)nk * (tiles <= 256 ? c.alone : c.full) + c.end + (act == CDL_ACT_GELU ? c.gelu : 0.0f) + (kept ? c.kept : 0.0f));
 }
+// The order of a product's sums (of parts, of a block's waves, or of K-tiles one after the other, which all forms of tiles have alike) does not go by `kept`: a call that stores z, for a step whose
+// forward pass is formed again, gives the y of the call that does not, bit for bit.  Which tiles does go by it.
 Choice choose(int32_t M, int32_t N, int32_t K, bool gated, int y_type, int act, bool kept)
 {
     if (K == 0) return {kParts, 0};
     const bool exact = y_type == CDL_F32;
     const int nk = (int)(block8_pitch(K) / kRingRow);
-    Choice best{kParts, 0};
-    float least = block8_parts_us(M, N, K) * (gated ? 2.0f : 1.0f) * (exact ? 1.5f : 1.0f);
+    Choice best{kParts, 0}, tiles{kSmall, 0};
+    float least = block8_parts_us(M, N, K) * (gated ? 2.0f : 1.0f) * (exact ? 1.5f : 1.0f), least_tiles = INFINITY;
+    bool by_tiles = false;
     for (const Way way : {kSmall, kPair, kWide}) {
         if (way == kWide && exact && !gated) continue;      // (it spills)
-        const float us = tiles_us(way, gated, exact, M, N, nk, act, kept);
-        if (us < least) {
-            least = us;
-            best.way = way;
+        const float bare = tiles_us(way, gated, exact, M, N, nk, act, false), us = kept ? tiles_us(way, gated, exact, M, N, nk, act, true) : bare;
+        if (us < least_tiles) {
+            least_tiles = us;
+            tiles.way = way;
+        }
+        if (bare < least) {
+            least = bare;
+            by_tiles = true;
         }
     }
+    if (by_tiles) best = tiles;
     for (const int rows : {1, 2, 4}) {
         const int64_t across = ((int64_t)M + 16 * rows - 1) / (16 * rows), blocks = ((int64_t)N + 15) / 16 * across;
         const float read = (float)((gated ? 2 : 1) + rows);      // sixteens of a block
@@ -136,11 +146,10 @@ size_t parts_bytes(int32_t M, int32_t N, int32_t K) { return align_up((size_t)bl
 size_t block8_gemm_act_workspace_bytes(int32_t M, int32_t N, int32_t K, bool gated)
 {
     if (M == 0 || N == 0 || K == 0) return 0;
-    // (whatever the results' type, the activation and what is kept, which the query does not know)
+    // (whatever the results' type and the activation, which the query does not know)
     for (const int type : {CDL_BF16, CDL_F32})
         for (const int act : {CDL_ACT_NONE, CDL_ACT_GELU})
-            for (const bool kept : {false, true})
-                if (choose(M, N, K, gated, type, act, kept).way == kParts) return parts_bytes(M, N, K) * (gated ? 2 : 1);
+            if (choose(M, N, K, gated, type, act, false).way == kParts) return parts_bytes(M, N, K) * (gated ? 2 : 1);
     return 0;
 }
 

@@ -1,0 +1,40 @@
+"""What a call of a feed-forward sublayer launches may depend on its sizes, not on which outputs it has: without a GPU."""
+import itertools
+
+import pytest
+
+import launch_recorder
+from launch_recorder import A, INT, POINTER, SIZE
+
+F32, BF16, E4M3 = 0, 1, 0
+NONE, RELU, GELU, SILU = 0, 1, 2, 3
+WS = [(POINTER, A), (SIZE, 1 << 60), (POINTER, None)]
+
+
+def product(M, N, K, y_type, act, sides, kept):
+    """`kept`: which results before the activation are asked for"""
+    name = "cdl_block8_gemm_act" if sides == 1 else "cdl_block8_gemm_gated"
+    z = [(POINTER, A if k else None) for k in kept]
+    tail = [(POINTER, A), (INT, act), (POINTER, A), (POINTER, A)] if sides == 1 else [(POINTER, A), (POINTER, A), (INT, act), (POINTER, A)]
+    return (name, [(POINTER, A)] * (2 + 2 * sides) + [(INT, v) for v in (M, N, K, E4M3, E4M3)] + tail + z + [(INT, y_type)] + WS)
+
+
+def order(launches):
+    """The order in which a product's sums are formed: of parts of the contraction in memory, of eight waves in a block, or of K-tiles one after the other, which all tiles have alike."""
+    names = [l.name for l in launches]
+    return "parts" if "finish" in names[-1] else "thin" if "thin" in names[0] else "tiles"
+
+
+# among them sizes whose estimates of two ways lie within what storing z adds to one of them
+SIZES = list(itertools.product((1, 16, 40, 64, 96, 128, 200, 300, 512, 1000, 2048, 4096, 9000), (100, 512, 768, 1024, 2048, 4096, 8192), (128, 512, 768, 1024, 2048, 4096, 8192, 32768)))
+
+
+@pytest.mark.parametrize("sides", [1, 2])
+@pytest.mark.parametrize("y_type", [F32, BF16])
+def test_the_order_of_sums_does_not_go_by_what_is_kept(tmp_path, sides, y_type):
+    choices = [(False,), (True,)] if sides == 1 else list(itertools.product((False, True), repeat=2))
+    for act in (NONE, GELU, SILU):
+        seen = [[order(launches) for launches, _ in launch_recorder.record(tmp_path, [product(*size, y_type, act, sides, kept) for size in SIZES])] for kept in choices]
+        assert {"parts", "thin", "tiles"} <= set(seen[0])
+        off = [size for i, size in enumerate(SIZES) if len({s[i] for s in seen}) > 1]
+        assert not off, (act, len(off), off[:10])

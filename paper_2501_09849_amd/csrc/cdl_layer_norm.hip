@@ -4,7 +4,8 @@
 //   h = g w:   d_x = r (h - mean of h - c mean of (h c)) + add,     d_w = sum over rows of g c,     d_b = sum over rows of g
 //
 // A row stays in the registers of L lanes, C chunks of eight entries each, so that it is read once: the mean, then the squares about it (a sum of squares less the mean's square would
-// lose rows far from zero), then the results.  Lanes that are not a whole block are a wave or a quarter of one, and their sums never leave the registers.  Weights, and backward the sums over the rows, stay
+// lose rows far from zero), then the results.  The mean's own roundings would enter every entry alike, times r (rows of 1000.1 and no spread came out 0.06 off their bias): it is the first
+// entry and the mean of the differences from it, which are all zero in such a row, and what it is still off is the mean of the differences from it, summed beside their squares.  Lanes that are not a whole block are a wave or a quarter of one, and their sums never leave the registers.  Weights, and backward the sums over the rows, stay
 // in registers too, so a team takes row after row, the next one's loads under way.
 // Bound by memory, 65536 x 768 in bf16: forward with the copy in eight bits 53 us (252 MB, 4.7 TB/s where a copy reaches 5.2), without 40; backward from eight bits onto a residual 70 us
 // (353 MB, 5.0 TB/s), from bf16 77, and 4 us for adding up the blocks' sums in a launch of their own.  2000 x 16384: forward 28 us, backward 77.
@@ -77,7 +78,9 @@ void layer_norm_fwd_kernel(NormFwd a)
     const int64_t step = (int64_t)gridDim.x * kTeams;
     int64_t row = (int64_t)blockIdx.x * kTeams + team;
     Raw8<T> raw[C];
+    T raw_first;
     auto fetch = [&](int64_t r) {
+        raw_first = ((const T *)a.x)[r * a.cols];
 #pragma unroll
         for (int c = 0; c < C; ++c) raw[c] = load_raw<RAGGED>((const T *)a.x + r * a.cols + (c * L + lane) * 8, left[c], a.stream, a.cols < 8);
     };
@@ -87,14 +90,18 @@ void layer_norm_fwd_kernel(NormFwd a)
             float v[C][8];
 #pragma unroll
             for (int c = 0; c < C; ++c) unpack<RAGGED>(raw[c], left[c], a.cols < 8, v[c]);
+            const float first = (float)raw_first;
             if (row + step < a.rows) fetch(row + step);
             float sum[1] = {0.0f};
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c) {
+                float part = 0.0f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) sum[0] += v[c][k];
+                for (int k = 0; k < 8; ++k) part += !RAGGED || k < left[c] ? v[c][k] - first : 0.0f;
+                sum[0] += left[c] > 0 ? part : 0.0f;
+            }
             row_sums<L>(sum, 0);
-            const float mean = sum[0] * a.by_cols;
+            const float near = __builtin_fmaf(sum[0], a.by_cols, first);
             if (KEEP) {
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
@@ -113,21 +120,27 @@ void layer_norm_fwd_kernel(NormFwd a)
                     }
                 }
             }
-            float square[1] = {0.0f};
+            float about[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c) {
+                float part[2] = {0.0f, 0.0f};
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    v[c][k] = (RAGGED ? k < left[c] : left[c] > 0) ? v[c][k] - mean : 0.0f;
-                    square[0] = __builtin_fmaf(v[c][k], v[c][k], square[0]);
+                    v[c][k] = !RAGGED || k < left[c] ? v[c][k] - near : 0.0f;
+                    part[0] += v[c][k];
+                    part[1] = __builtin_fmaf(v[c][k], v[c][k], part[1]);
                 }
-            row_sums<L>(square, 1);
-            const float rstd = 1.0f / sqrtf(square[0] * a.by_cols + a.eps);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) about[i] += left[c] > 0 ? part[i] : 0.0f;
+            }
+            row_sums<L>(about, 1);
+            const float off = about[0] * a.by_cols, var = __builtin_fmaf(-off, off, about[1] * a.by_cols), mean = near + off;
+            const float rstd = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + a.eps);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 float y[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) y[k] = __builtin_fmaf(v[c][k] * rstd, w[c][k], b[c][k]);
+                for (int k = 0; k < 8; ++k) y[k] = __builtin_fmaf((v[c][k] - off) * rstd, w[c][k], b[c][k]);
                 store_first<RAGGED>((T *)a.y + row * a.cols + (c * L + lane) * 8, left[c], y, a.stream);
             }
             if (lane == 0) {

@@ -51,3 +51,72 @@ def test_a_forward_pass_formed_again_with_z(env, size, sides, kind):
             assert torch.equal(got, want), (name, kept)
             all_z = all_z or z
             assert all(torch.equal(p, q) for p, q, k in zip(z, all_z, kept) if k)
+
+
+# ---- layer norm: rows whose mean is large beside their spread ----------------------------------------------------------
+
+WIDTHS = [1, 7, 100, 128, 300, 513, 768, 1000, 1021, 1025, 2047, 3001, 4096, 8200, 16376, 16384]      # every number of lanes and chunks, whole and ragged
+
+
+def norm_fwd(torch, cdl, x, w=None, b=None, eps=1e-5, keep=False):
+    rows, cols = x.shape
+    y, mean, rstd = torch.full_like(x, float("nan")), torch.full((rows,), float("nan"), device="cuda"), torch.full((rows,), float("nan"), device="cuda")
+    q, scale = su.empty8(torch, rows, cols) if keep else (None, None)
+    cdl.cdl_layer_norm_fwd(x, rows, cols, y, mean, rstd, weight=w, bias=b, eps=eps, q=q, scale=scale)
+    torch.cuda.synchronize()
+    return y, mean, rstd
+
+
+def norm_bounds(torch, x, w, b, eps, kind):
+    """[(result, error)] of y, mean and rstd.  A sum of a row is 32 entries in a lane and 4 + 2 + 8 joins, less than 64 roundings.  The mean first formed is off by its own rounding and by that
+    of the sum of differences from the first entry; what is subtracted in the end is the mean of differences from it, so that is all that is left of either."""
+    U = su.U
+    mean = x.mean(dim=1, keepdim=True)
+    c = x - mean
+    var, size = (c * c).mean(dim=1, keepdim=True), c.abs().mean(dim=1, keepdim=True)
+    first = U * mean.abs() + 68 * U * (x - x[:, :1]).abs().mean(dim=1, keepdim=True)
+    off_c = 2 * U * c.abs() + U * first + 66 * U * (size + first)
+    rstd = 1 / torch.sqrt(var + eps)
+    off_var = 68 * U * (var + 2 * first * first) + 2 * first * 66 * U * (size + first)
+    off_r = rstd * (0.5 * off_var / (var + eps) + 4 * U)
+    y = c * rstd * w + b
+    off_y = w.abs() * (off_c * rstd + c.abs() * off_r + 2 * U * c.abs() * rstd) + U * y.abs() + su.HALF[kind] * y.abs() + su.TINY
+    return (y, off_y), (mean[:, 0], (U * mean.abs() + 66 * U * (size + first))[:, 0]), (rstd[:, 0], off_r[:, 0])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_rows_of_one_value_are_the_bias(env, cols, kind):
+    """No difference from the first entry has a rounding: the mean is the value, y the bias; with eps 0 there is no norm."""
+    torch, cdl = env
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    values = [1000.1, 0.1, 100.0, 1000.0, 3.0, -30000.3, 0.0, 1e-20]
+    x = torch.tensor(values, device="cuda")[:, None].expand(-1, cols).contiguous().to(getattr(torch, kind))
+    w, b = torch.randn(cols, device="cuda", generator=gen), torch.randn(cols, device="cuda", generator=gen)
+    for keep in (False, True):
+        y, mean, rstd = norm_fwd(torch, cdl, x, w, b, keep=keep)
+        assert torch.equal(mean, x[:, 0].float()) and torch.equal(y, b.to(x.dtype).expand_as(y))
+        assert float((rstd.double() * 1e-5 ** 0.5 - 1).abs().max()) <= 4 * su.U
+        y, mean, rstd = norm_fwd(torch, cdl, x, w, b, eps=0.0, keep=keep)
+        assert torch.equal(mean, x[:, 0].float()) and torch.isnan(y).all() and torch.isinf(rstd).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("cols", WIDTHS[1:])
+def test_the_mean_adds_nothing_to_the_rows(env, cols, kind):
+    """Rows whose mean is up to 10^5 times their spread, rows with a spread of a few units of their last place, rows whose first entry is far from all others."""
+    torch, cdl = env
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    r = lambda *s: torch.randn(s, device="cuda", generator=gen)      # noqa: E731
+    x = r(64, cols)
+    x[:16] += 1000.1
+    x[16:24] = x[16:24] * 1e-2 + 1000.1
+    x[24:32] = 1000.1 + 6.104e-5 * torch.randint(0, 3, (8, cols), device="cuda", generator=gen)
+    x[32:40, 0] = 1e4
+    x[40:48] = x[40:48] * 1e-3 - 0.1
+    x[48:52, 0] += 1e6
+    x = x.to(getattr(torch, kind))
+    w, b = 1 + 0.2 * r(cols), 0.2 * r(cols)
+    for eps in (1e-5, 1e-12):
+        for got, want in zip(norm_fwd(torch, cdl, x, w, b, eps), norm_bounds(torch, x.double(), w.double(), b.double(), eps, kind)):
+            assert su.outside(got, *want) == 0, eps

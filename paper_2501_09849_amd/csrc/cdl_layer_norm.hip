@@ -325,10 +325,10 @@ int64_t fwd_blocks(int form, int64_t rows)
 }
 // Backward: as many rows for every team, on the blocks that a compute unit holds two of, or one where a block has one row at a time and a thread many registers.  More blocks leave more
 // sums to be added up, and rows that do not come out even (65536 x 768 from eight bits: 384 blocks 82.4 us, 512 71.6, 768 73.7, 1024 81.6; 4096 x 8192: 256 blocks 61.2, 512 70.0).
-// Few rows are one block's, which has the sums without a second launch (16 x 768: 6.9 us instead of 8.9).
-int64_t bwd_blocks(int form, int64_t rows)
+// Sums of few rows are one block's, which has them without a second launch (16 x 768: 6.9 us instead of 8.9); where none are asked for, every team has a row as long as there are blocks.
+int64_t bwd_blocks(int form, int64_t rows, bool sums)
 {
-    if (rows <= 4 * teams_of(form)) return 1;
+    if (sums && rows <= 4 * teams_of(form)) return 1;
     const int64_t teams = teams_of(form), most = teams == 1 && kChunksOf[form] > 1 ? 256 : 512, per = (rows + most * teams - 1) / (most * teams);
     return (rows + per * teams - 1) / (per * teams);
 }
@@ -360,7 +360,7 @@ int launch_bwd(const NormBwd &a, hipStream_t stream)
     static const kernel_t kernels[kForms] = {layer_norm_bwd_kernel<T, 16, 1, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 16, 2, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 64, 1, RAGGED, KEPT>,
                                              layer_norm_bwd_kernel<T, 64, 2, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 256, 1, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 256, 2, RAGGED, KEPT>,
                                              layer_norm_bwd_kernel<T, 256, 4, RAGGED, KEPT>, layer_norm_bwd_kernel<T, 512, 4, RAGGED, KEPT>};
-    CDL_LAUNCH("layer_norm_bwd_kernel", stream, kernels[form], dim3((unsigned)bwd_blocks(form, a.rows)), dim3(kLanes[form] > 256 ? kLanes[form] : 256), 0, a);
+    CDL_LAUNCH("layer_norm_bwd_kernel", stream, kernels[form], dim3((unsigned)bwd_blocks(form, a.rows, a.parts || a.sums[0] || a.sums[1])), dim3(kLanes[form] > 256 ? kLanes[form] : 256), 0, a);
     return check_launch();
 }
 template <class T>
@@ -385,16 +385,17 @@ int launch_layer_norm_fwd(const void *x, int32_t type, const float *weight, cons
 
 size_t layer_norm_bwd_workspace_bytes(int32_t rows, int32_t cols)
 {
-    if (rows == 0 || bwd_blocks(form_of(cols), rows) == 1) return 0;
-    return align_up((size_t)bwd_blocks(form_of(cols), rows) * 2 * (size_t)part_cols(cols) * sizeof(float), 256);
+    if (rows == 0 || bwd_blocks(form_of(cols), rows, true) == 1) return 0;
+    return align_up((size_t)bwd_blocks(form_of(cols), rows, true) * 2 * (size_t)part_cols(cols) * sizeof(float), 256);
 }
 
 int launch_layer_norm_bwd(const void *g, int32_t type, const void *x, const uint8_t *q, const uint8_t *scale, int32_t format, const float *weight, const float *mean,
                           const float *rstd, const void *add, int32_t rows, int32_t cols, void *d_x, float *d_weight, float *d_bias, void *ws, hipStream_t stream)
 {
-    const int64_t blocks = rows > 0 ? bwd_blocks(form_of(cols), rows) : 0;
+    const bool sums = d_weight || d_bias;
+    const int64_t blocks = rows > 0 ? bwd_blocks(form_of(cols), rows, sums) : 0;
     const bool at_once = blocks == 1;
-    float *const parts = (d_weight || d_bias) && !at_once ? (float *)ws : nullptr;
+    float *const parts = sums && !at_once ? (float *)ws : nullptr;
     const int64_t size = type == CDL_BF16 ? 2 : 4;
     if (rows > 0) {
         const NormBwd a{g, x, q, scale, weight, mean, rstd, add, rows, cols, 1.0f / (float)cols, d_x, parts, {at_once ? d_weight : nullptr, at_once ? d_bias : nullptr}, block8_pitch(cols), block8_pitch(rows), part_cols(cols),
@@ -403,7 +404,7 @@ int launch_layer_norm_bwd(const void *g, int32_t type, const void *x, const uint
         const int rc = type == CDL_BF16 ? launch_bwd<bf16_t>(a, kept, stream) : launch_bwd<float>(a, kept, stream);
         if (rc != CDL_OK) return rc;
     }
-    if ((!d_weight && !d_bias) || at_once) return CDL_OK;
+    if (!sums || at_once) return CDL_OK;
     return launch_column_sums(parts, blocks, cols, part_cols(cols), d_weight, d_bias, stream);
 }
 

@@ -120,3 +120,23 @@ def test_the_mean_adds_nothing_to_the_rows(env, cols, kind):
     for eps in (1e-5, 1e-12):
         for got, want in zip(norm_fwd(torch, cdl, x, w, b, eps), norm_bounds(torch, x.double(), w.double(), b.double(), eps, kind)):
             assert su.outside(got, *want) == 0, eps
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,cols", [(1, 16384), (4, 16384), (3, 8001), (16, 1024), (15, 769), (64, 128), (61, 100), (700, 300)])
+def test_a_gradient_alone_is_that_of_a_call_with_sums(env, rows, cols, kind):
+    """(few rows of a call with sums are one block's, of one without they are not)"""
+    torch, cdl = env
+    gen = torch.Generator(device="cuda").manual_seed(rows + cols)
+    x, g, add = (torch.randn((rows, cols), device="cuda", generator=gen).to(getattr(torch, kind)) for _ in range(3))
+    w = torch.randn(cols, device="cuda", generator=gen)
+    _, mean, rstd = norm_fwd(torch, cdl, x)
+    got = [torch.full_like(x, float("nan")) for _ in range(2)]
+    sums = [torch.full((cols,), float("nan"), device="cuda") for _ in range(2)]
+    ws = torch.empty(max(256, cdl.layer_norm_bwd_workspace_bytes(rows, cols)), dtype=torch.uint8, device="cuda")
+    for given in (dict(x=x), dict(zip(("q", "scale"), su.quantize(torch, cdl, x)))):
+        cdl.cdl_layer_norm_bwd(g, rows, cols, mean, rstd, d_x=got[0], weight=w, add=add, **given)
+        cdl.cdl_layer_norm_bwd(g, rows, cols, mean, rstd, d_x=got[1], d_weight=sums[0], d_bias=sums[1], weight=w, add=add, ws=ws, **given)
+        at = su.values(torch, given["q"], given["scale"], cols=cols) if "q" in given else x.double()
+        wants = su.norm_back(torch, g.double(), at, w, mean, rstd, add.double(), kind)
+        assert torch.equal(*got) and [su.outside(v, *want) for v, want in zip([got[0]] + sums, wants)] == [0, 0, 0]

@@ -38,3 +38,17 @@ def test_the_order_of_sums_does_not_go_by_what_is_kept(tmp_path, sides, y_type):
         assert {"parts", "thin", "tiles"} <= set(seen[0])
         off = [size for i, size in enumerate(SIZES) if len({s[i] for s in seen}) > 1]
         assert not off, (act, len(off), off[:10])
+
+
+@pytest.mark.parametrize("type_", [F32, BF16])
+def test_rows_of_a_gradient_alone_are_not_one_block(tmp_path, type_):
+    """Few rows are one block's for the sake of their sums (weight, bias).  The gradient of x alone takes the blocks that its rows fill."""
+    def call(rows, cols, d_weight, d_bias):
+        return ("cdl_layer_norm_bwd", [(POINTER, A), (INT, type_), (POINTER, A), (POINTER, None), (POINTER, None), (INT, 0)] + [(POINTER, A)] * 4 + [(INT, rows), (INT, cols), (POINTER, A),
+                (POINTER, d_weight), (POINTER, d_bias)] + WS)
+    sizes = {(64, 128): 4, (64, 256): 4, (16, 512): 4, (16, 1024): 4, (15, 768): 4, (4, 2048): 4, (4, 4096): 4, (3, 8000): 3, (4, 16384): 4, (1, 16384): 1, (600, 300): 150, (5000, 16384): 250}
+    for d_weight, d_bias in ((None, None), (A, A), (A, None), (None, A)):
+        for ((rows, cols), blocks), (launches, _) in zip(sizes.items(), launch_recorder.record(tmp_path, [call(*size, d_weight, d_bias) for size in sizes])):
+            some = d_weight or d_bias
+            few = some and rows <= 64
+            assert launches[0].grid[0] == (1 if few else blocks) and len(launches) == (2 if some and not few else 1), (rows, cols)

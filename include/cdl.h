@@ -479,7 +479,8 @@ int cdl_dropout(const void *x, const void *add, int32_t type, int64_t n, float p
  *
  * Tensors are of `type` (CDL_F32, CDL_BF16), 16-byte aligned, as are the fp32 vectors of weights and biases; all sums, means and activations are formed in fp32
  * and each output is rounded once.  Same inputs, same bits.  Outputs share no memory with inputs or with each other, unless it says so.  An entry that is not
- * finite makes what its row (layer norm), its entry (activations) or its column (sums over the rows) holds not finite, and nothing else.
+ * finite makes what its row (layer norm), its entry (activations) or its column (sums over the rows) holds not finite, and nothing else - but max(z, 0) and its
+ * derivative are 0 at minus infinity, and where there is no activation the derivative is 1 whatever z is.
  *
  * Activations kept in eight bits.  Where a backward pass takes (q, scale, format) in the place of a tensor of `type`, these are its rows as cdl_block8_quantize writes
  * them without tiles - q [rows][pitch(cols)], scale [blocks of cols][pitch(rows)], bytes 1 .. 254, or 255 for a block that is not finite -, half of the memory of bf16,
@@ -490,7 +491,8 @@ int cdl_dropout(const void *x, const void *add, int32_t type, int64_t n, float p
  * Layer norm of the rows of x[rows, cols]:  y = (x - mean) rstd * weight + bias,  rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
  *   weight, bias  fp32[cols], nullable (1 and 0);   y [rows, cols];   mean, rstd  fp32[rows], nullable
  *   q, scale      nullable: x in eight bits for the backward pass, in the same pass over x and byte for byte what cdl_block8_quantize gives
- * What y is off goes with the spread of its row, not with its mean: a row of equal entries is the bias (eps 0: not finite).  y may be x.  cols >= 1 unless rows == 0, eps finite and not negative (CDL_ERR_PARAM); CDL_ERR_RANGE for cols > 16384, rows > 2^30 or rows * cols > 2^44.
+ * What y is off goes with the spread of its row, not with its mean: a row of equal entries is the bias (eps 0: not finite).  The squares are fp32 too: a row of which they pass the largest
+ * number has rstd 0.  y may be x.  cols >= 1 unless rows == 0, eps finite and not negative (CDL_ERR_PARAM); CDL_ERR_RANGE for cols > 16384, rows > 2^30 or rows * cols > 2^44.
  */
 int cdl_layer_norm_fwd(const void *x, int32_t type, const float *weight, const float *bias, int32_t rows, int32_t cols, float eps,
                        void *y, float *mean, float *rstd, uint8_t *q, uint8_t *scale, int32_t format, void *hip_stream);

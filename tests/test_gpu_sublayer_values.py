@@ -140,3 +140,69 @@ def test_a_gradient_alone_is_that_of_a_call_with_sums(env, rows, cols, kind):
         at = su.values(torch, given["q"], given["scale"], cols=cols) if "q" in given else x.double()
         wants = su.norm_back(torch, g.double(), at, w, mean, rstd, add.double(), kind)
         assert torch.equal(*got) and [su.outside(v, *want) for v, want in zip([got[0]] + sums, wants)] == [0, 0, 0]
+
+
+# ---- what is not finite ----------------------------------------------------------------------------------------------
+
+INF, NAN = float("inf"), float("nan")
+# value and derivative at minus infinity, infinity and no number
+VALUES = {"none": [-INF, INF, NAN], "relu": [0.0, INF, NAN], "gelu": [NAN, INF, NAN], "silu": [NAN, INF, NAN]}
+SLOPES = {"none": [1.0, 1.0, 1.0], "relu": [0.0, 1.0, NAN], "gelu": [NAN, NAN, NAN], "silu": [NAN, NAN, NAN]}
+
+
+def same(torch, got, wants):
+    """each of `got` against one number"""
+    return all((torch.isnan(v) if want != want else v.double() == want).all() for v, want in zip(got, wants))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("name", su.ACTS)
+def test_gradients_where_z_is_not_finite(env, name, kind):
+    """z as it is: its own entry; as kept in eight bits: no number for the 128 entries of its block"""
+    torch, cdl = env
+    t, at = getattr(torch, kind), [5, 130, 299]
+    for rows, cols in ((3, 300), (50, 301), (500, 300)):
+        gen = torch.Generator(device="cuda").manual_seed(rows)
+        g, z, up = ((torch.rand((rows, cols), device="cuda", generator=gen) + 0.5).to(t) for _ in range(3))
+        z[1, at] = torch.tensor([-INF, INF, NAN], device="cuda", dtype=t)
+        d, y, bias = torch.empty_like(g), torch.empty_like(g), torch.empty(cols, device="cuda")
+        ws = torch.empty(max(256, cdl.gated_bwd_workspace_bytes(rows, cols)), dtype=torch.uint8, device="cuda")
+        act = su.number(cdl, name)
+        cdl.cdl_act_bwd(g, rows, cols, act, d_z=d, d_bias=bias, y=y, z=z, ws=ws)
+        slopes, values = SLOPES[name], VALUES[name]
+        assert same(torch, d[1, at], [s * float(v) for s, v in zip(slopes, g[1, at])]) and same(torch, y[1, at], values)
+        rest = torch.ones_like(z, dtype=torch.bool)
+        rest[1, at] = False
+        assert torch.isfinite(d[rest]).all() and torch.isfinite(y[rest]).all()
+        assert [bool(torch.isfinite(v)) for v in bias[at]] == [s == s for s in slopes] and int(torch.isfinite(bias).sum()) == cols - sum(s != s for s in slopes)
+        d_up = torch.empty_like(g)
+        cdl.cdl_gated_bwd(g, rows, cols, act, d_gate=d, d_up=d_up, y=y, z_gate=z, z_up=up)
+        assert same(torch, d_up[1, at], [v * float(f) for v, f in zip(values, g[1, at])]) and same(torch, y[1, at], [v * float(f) for v, f in zip(values, up[1, at])])
+        assert [bool(torch.isfinite(v)) for v in d[1, at]] == [s == s for s in slopes]
+        assert torch.isfinite(d[rest]).all() and torch.isfinite(d_up[rest]).all() and torch.isfinite(y[rest]).all()
+        q, scale = su.quantize(torch, cdl, z)
+        cdl.cdl_act_bwd(g, rows, cols, act, d_z=d, y=y, q=q, scale=scale)
+        hit = torch.zeros_like(rest)
+        hit[1] = True      # (each block of the row has one)
+        assert torch.isnan(y[hit]).all() and torch.isfinite(y[~hit]).all() and torch.isfinite(d[~hit]).all()
+        assert torch.equal(d, g) if name == "none" else torch.isnan(d[hit]).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("name", su.ACTS)
+@pytest.mark.parametrize("size", [(2, 300, 0), (2, 300, 200), (300, 401, 9000), (1021, 1000, 520), (2000, 1999, 520), (3000, 2900, 384)])
+def test_products_where_z_is_not_finite(env, size, name, kind):
+    torch, cdl = env
+    M, N, K = size
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    a, w = (su.quantize(torch, cdl, torch.randn((n, max(K, 1)), device="cuda", generator=gen) * max(K, 1) ** -0.5) for n in (M, N))
+    bias, at = torch.rand(N, device="cuda", generator=gen) + 0.5, [0, N // 2, N - 1]
+    bias[at] = torch.tensor([-INF, INF, NAN], device="cuda")
+    rest = torch.ones(N, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    for kept in (False, True):
+        y, (z,) = finished(torch, cdl, a, [w], size, kind, name, [bias], [kept])
+        assert same(torch, y.t()[at], VALUES[name]) and torch.isfinite(y[:, rest]).all()
+        assert not kept or (same(torch, z.t()[at], VALUES["none"]) and torch.isfinite(z[:, rest]).all())
+        y, _ = finished(torch, cdl, a, [w, w], size, kind, name, [bias, torch.ones(N, device="cuda") * 1000], [kept, kept])      # (z of the other projection: positive)
+        assert same(torch, y.t()[at], VALUES[name]) and torch.isfinite(y[:, rest]).all()

@@ -206,3 +206,41 @@ def test_products_where_z_is_not_finite(env, size, name, kind):
         assert not kept or (same(torch, z.t()[at], VALUES["none"]) and torch.isfinite(z[:, rest]).all())
         y, _ = finished(torch, cdl, a, [w, w], size, kind, name, [bias, torch.ones(N, device="cuda") * 1000], [kept, kept])      # (z of the other projection: positive)
         assert same(torch, y.t()[at], VALUES[name]) and torch.isfinite(y[:, rest]).all()
+
+
+# ---- exact products --------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("sides", [1, 2])
+@pytest.mark.parametrize("fa,fb", [("e4m3", "e4m3"), ("e5m2", "e4m3")])
+@pytest.mark.parametrize("size", [(1, 48, 300), (3, 1000, 2048), (40, 333, 1300), (64, 4096, 4096), (96, 4096, 512), (300, 401, 9000), (129, 250, 9000), (256, 256, 30000), (1021, 1000, 520), (2000, 1999, 520), (3000, 3001, 200),
+                                  (9000, 4000, 256)])
+def test_results_in_fp32_leave_nothing_out(env, size, fa, fb, sides):
+    """Products of 2^-8 beside one of 2^8 in every 128: each sum and partial sum is a multiple of 2^-8 below 2^16, a number of fp32 whatever the order, so the results are exact.  The instructions
+    for eight bits keep of eight products or more at a time what lies above 2^-14 of the largest: they lose those of 2^-8 beside the large one, which leaves four entries of five off."""
+    torch, cdl = env
+    M, N, K = size
+    gen = torch.Generator(device="cuda").manual_seed(M + N + K)
+
+    def matrix(rows, fmt, sign):
+        x = (torch.randint(0, 2, (rows, K), device="cuda", generator=gen) * 2 - 1).float() * 2.0 ** -4
+        x[:, 37::128] = 16.0
+        x[:, 36::128] = 2.0 ** -4 * sign
+        return su.quantize(torch, cdl, x, fmt), x.double()
+    a, va = matrix(M, fa, 1)
+    b = [matrix(N, fb, 1 - 2 * i) for i in range(sides)]
+    wants = [va @ v.t() for _, v in b]
+    assert all(float(w.abs().max()) < 2.0 ** 16 for w in wants)
+    new = lambda: torch.full((M, N), float("nan"), device="cuda")      # noqa: E731
+    query = cdl.block8_gemm_act_workspace_bytes if sides == 1 else cdl.block8_gemm_gated_workspace_bytes
+    y, z, ws = new(), [new() for _ in b], torch.full((max(256, query(M, N, K)),), 0xff, dtype=torch.uint8, device="cuda")
+    fmt = {"e4m3": cdl.E4M3, "e5m2": cdl.E5M2}
+    more = dict(act=cdl.ACT_RELU, ws=ws, a_format=fmt[fa], b_format=fmt[fb])
+    for keep in (True, False):
+        y.fill_(float("nan"))
+        if sides == 1:
+            cdl.cdl_block8_gemm_act(*a, *b[0][0], M, N, K, y, z=z[0] if keep else None, **more)
+            want = wants[0].clamp(min=0)
+        else:
+            cdl.cdl_block8_gemm_gated(*a, *b[0][0], *b[1][0], M, N, K, y, z_gate=z[0] if keep else None, z_up=z[1] if keep else None, **more)
+            want = (wants[0].clamp(min=0) * wants[1]).float().double()      # (one rounding)
+        assert all(torch.equal(p.double(), w) for p, w in zip(z, wants)) and torch.equal(y.double(), want)

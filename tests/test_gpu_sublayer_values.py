@@ -244,3 +244,57 @@ def test_results_in_fp32_leave_nothing_out(env, size, fa, fb, sides):
             cdl.cdl_block8_gemm_gated(*a, *b[0][0], *b[1][0], M, N, K, y, z_gate=z[0] if keep else None, z_up=z[1] if keep else None, **more)
             want = (wants[0].clamp(min=0) * wants[1]).float().double()      # (one rounding)
         assert all(torch.equal(p.double(), w) for p, w in zip(z, wants)) and torch.equal(y.double(), want)
+
+
+# ---- sums over the rows of tensors whose offsets pass 32 bits ----------------------------------------------------------
+
+ROWS, COLS = 1050000, 4101      # more than 2^32 entries
+
+
+def large(torch, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.empty((ROWS, COLS), dtype=torch.bfloat16, device="cuda")
+    for first in range(0, ROWS, 1 << 17):
+        x[first:first + (1 << 17)] = torch.randn((min(1 << 17, ROWS - first), COLS), device="cuda", generator=gen)
+    return x
+
+
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("sides", [1, 2])
+def test_sums_of_large_activations(env, sides, kept):
+    """The gradients of slices are those of calls on the slices, the sums those of all rows in 64 bits."""
+    torch, cdl = env
+    g, z = large(torch, 1), [large(torch, 2 + i) for i in range(sides)]
+    if kept:
+        z = [su.quantize(torch, cdl, z.pop()) for _ in range(sides)]
+    bias = [torch.full((COLS,), float("nan"), device="cuda") for _ in range(sides)]
+    query = cdl.act_bwd_workspace_bytes if sides == 1 else cdl.gated_bwd_workspace_bytes
+    ws = torch.empty(query(ROWS, COLS), dtype=torch.uint8, device="cuda")
+
+    def call(g, z, rows, **out):
+        names = [""] if sides == 1 else ["_gate", "_up"]
+        given = {k + n: t for n, v in zip(names, z) for k, t in zip(("q", "scale") if kept else ("z",), v if kept else (v,))}
+        out = {("d_z" if sides == 1 else "d") + n if k == "d" else k + n: t for k, v in out.items() if k != "ws" for n, t in zip(names, v)}
+        (cdl.cdl_act_bwd if sides == 1 else cdl.cdl_gated_bwd)(g, rows, COLS, cdl.ACT_SILU, ws=ws, **given, **out)
+    d = [torch.empty_like(g) for _ in range(sides)]
+    call(g, z, ROWS, d=d, d_bias=bias)
+    part = lambda v, at: (v[0][at], v[1][:, at].contiguous()) if kept else v[at]      # noqa: E731
+    for first in (0, 523904, 1047168, 1049856):      # around 2^31 and 2^32 entries, and the last rows
+        n = min(256, ROWS - first)
+        of = [torch.empty((n, COLS), dtype=g.dtype, device="cuda") for _ in d]
+        at = slice(first, first + n)
+        some = [part(v, at) for v in z]
+        if kept and n % 128:
+            some = [(q, torch.nn.functional.pad(s, (0, -n % 128))) for q, s in some]
+        call(g[at], some, n, d=of)
+        assert all(torch.equal(t[at], p) for t, p in zip(d, of)), first
+    del d
+    sums, sizes = ([torch.zeros(COLS, dtype=torch.float64, device="cuda") for _ in range(sides)] for _ in range(2))
+    for first in range(0, ROWS, 1 << 16):
+        at = slice(first, min(first + (1 << 16), ROWS))
+        values = [su.values(torch, *part(v, at), cols=COLS) if kept else v[at].double() for v in z]
+        for i, (v, off) in enumerate(su.act_back(torch, "silu", g[at].double(), values, "float32")[0]):
+            sums[i] += v.sum(dim=0)
+            sizes[i] += off.sum(dim=0) + (ROWS / 121 / 8 + 40) * su.U * v.abs().sum(dim=0)      # 121 stretches of rows, an eighth of each one behind the other, then 8 + 2 + 18 sums
+    for got, want, off in zip(bias, sums, sizes):
+        assert su.outside(got, want, off) == 0

@@ -19,6 +19,9 @@ struct ThinJob {
 };
 
 constexpr int kThinWaves = 8;
+// Rows of a that a block takes at most, in sixteens.  Two projections' exact products with 64 rows do not fit the registers: 23 spilled in the loop, 64 x 2048 x 1536 gated took 9.4 us
+// (32 rows 5.4), 52 x 2000 x 3000 14.0 (8.4); where the loop is short it was as good or better, 64 x 4096 x 512 5.6 (6.0).
+constexpr int thin_most(bool gated, bool exact) { return gated && exact ? 2 : 4; }
 
 template <int FA, int FB, bool EXACT>
 __device__ __forceinline__ void thin_product(v4f &acc, const v8i &b, const v8i &a, int sb, int sa)
@@ -132,7 +135,7 @@ void block8_thin_kernel(ThinJob job)
 template <int FA, int FB, bool GATED, class T>
 int launch_thin(const ThinJob &job, int qt, hipStream_t stream)
 {
-    const auto kernel = qt == 1 ? block8_thin_kernel<FA, FB, GATED, 1, T> : qt == 2 ? block8_thin_kernel<FA, FB, GATED, 2, T> : block8_thin_kernel<FA, FB, GATED, 4, T>;
+    const auto kernel = qt == 1 ? block8_thin_kernel<FA, FB, GATED, 1, T> : qt == 2 ? block8_thin_kernel<FA, FB, GATED, 2, T> : block8_thin_kernel<FA, FB, GATED, thin_most(GATED, sizeof(T) == 4), T>;
     const dim3 grid((unsigned)((job.to.N + 15) / 16), (unsigned)((job.to.M + 16 * qt - 1) / (16 * qt)));
     CDL_LAUNCH(GATED ? "block8_gated_thin_kernel" : "block8_act_thin_kernel", stream, kernel, grid, dim3(kThinWaves * 64), 0, job);
     return check_launch();

@@ -128,6 +128,7 @@ Choice choose(int32_t M, int32_t N, int32_t K, bool gated, int y_type, int act, 
     }
     if (by_tiles) best = tiles;
     for (const int rows : {1, 2, 4}) {
+        if (rows > thin_most(gated, exact)) continue;
         const int64_t across = ((int64_t)M + 16 * rows - 1) / (16 * rows), blocks = ((int64_t)N + 15) / 16 * across;
         const float read = (float)((gated ? 2 : 1) + rows);      // sixteens of a block
         const float us = 3.5f + (float)blocks * 16.0f * read * (float)block8_pitch(K) / (exact ? 6e6f : 9e6f) + 0.2f * read * (float)((nk + 7) / 8) + (float)(blocks / 512);

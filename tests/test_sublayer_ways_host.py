@@ -1,5 +1,6 @@
 """What a call of a feed-forward sublayer launches may depend on its sizes, not on which outputs it has: without a GPU."""
 import itertools
+import re
 
 import pytest
 
@@ -52,3 +53,16 @@ def test_rows_of_a_gradient_alone_are_not_one_block(tmp_path, type_):
             some = d_weight or d_bias
             few = some and rows <= 64
             assert launches[0].grid[0] == (1 if few else blocks) and len(launches) == (2 if some and not few else 1), (rows, cols)
+
+
+@pytest.mark.parametrize("sides", [1, 2])
+@pytest.mark.parametrize("y_type", [F32, BF16])
+def test_blocks_of_few_rows(tmp_path, sides, y_type):
+    """16 to 64 rows of a in a block; exact products of two projections 32 at most, more would not fit the registers"""
+    rows = {2 if sides == 2 and y_type == F32 else 4}
+    seen = set()
+    for launches, _ in launch_recorder.record(tmp_path, [product(M, N, K, y_type, SILU, sides, (False,) * sides) for M in (1, 16, 20, 52, 64, 128) for N in (1000, 2048, 4096) for K in (500, 768, 1536, 3000)]):
+        if order(launches) == "thin":
+            form = re.search(r"(?:true|false), (\d)|Lb[01]ELi(\d)E", launches[0].name)      # (names with bf16 stay mangled)
+            seen.add(int(form.group(1) or form.group(2)))
+    assert {1, 2} <= seen and max(seen) in rows

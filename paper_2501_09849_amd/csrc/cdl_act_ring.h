@@ -4,7 +4,7 @@
 // What it costs: a wave of 128 x 128 is alone on its SIMD and issues the end of a tile in 7500 cycles, with silu in 12700, with gelu in 28600, where six K-tiles take 24500; its stores, one
 // behind the other with those of every other compute unit, take as long as memory takes (128 KB a tile and compute unit in 4.7 us at the 7.2 TB/s that all stores together reach in the caches), and
 // the loads of the next tile come in order behind them.  65536 x 4096 x 768 into bf16: 170 us products and loads alone, 270 with the stores, gelu 392 (in tiles of 128 x 128, where the other block
-// multiplies meanwhile, 363).  65536 x 2048 x 768 gated, all three results kept: 313 us, 805 MB written.
+// multiplies meanwhile, 363), gelu with z kept 452.  65536 x 2048 x 768 gated, all three results kept: 313 us, on other cards 322 to 332; 805 MB written.
 #pragma once
 
 #include "cdl_act.h"
@@ -282,7 +282,7 @@ void block8_act_kernel(RingCall<ActStore<FORM, T>> call)
 }
 
 // Tiles of 256 x 256, one block on a compute unit; of 128 x 128, two: while one finishes a tile, the other multiplies; of 64 x 64 (gated: 128 x 64, 64 of either matrix), two, with more
-// K-tiles under way: for products of so few tiles that their latency counts.
+// K-tiles under way: for products of so few tiles that their latency counts.  (The staging of the first two is what ring() asks for of rings of two; nothing is written there.)
 template <bool GATED> using ActWide = RingForm<2, 2, 4, 4, 2, 2, 1, 4096, true, GATED>;
 template <bool GATED> using ActPair = RingForm<2, 2, 2, 2, 2, 2, 2, 2048, true, GATED>;
 template <bool GATED> using ActSmall = std::conditional_t<GATED, RingForm<2, 2, 2, 1, 3, 3, 2, 0, true, true>, RingForm<2, 2, 1, 1, 4, 4, 2, 0, true, false>>;
@@ -309,7 +309,7 @@ int launch_act_ring(ActForm form, const RingJob &job, const ActTarget &to, int a
 {
     constexpr bool kExact = sizeof(T) == 4;
     if (form == ActForm::kSmall) return launch_act_form<ActSmall<GATED>, kExact, T>(job, to, a_format, b_format, stream);
-    if constexpr (!kExact || GATED) {      // (exact products in wide tiles spill where a tile has four accumulators a row: ring_us())
+    if constexpr (!kExact || GATED) {      // (exact products in wide tiles of one matrix spill: choose() does not take them)
         if (form == ActForm::kWide) return launch_act_form<ActWide<GATED>, kExact, T>(job, to, a_format, b_format, stream);
     }
     return launch_act_form<ActPair<GATED>, kExact, T>(job, to, a_format, b_format, stream);

@@ -7,8 +7,8 @@
 // lose rows far from zero), then the results.  The mean's own roundings would enter every entry alike, times r (rows of 1000.1 and no spread came out 0.06 off their bias): it is the first
 // entry and the mean of the differences from it, which are all zero in such a row, and what it is still off is the mean of the differences from it, summed beside their squares.  Lanes that are not a whole block are a wave or a quarter of one, and their sums never leave the registers.  Weights, and backward the sums over the rows, stay
 // in registers too, so a team takes row after row, the next one's loads under way.
-// Bound by memory, 65536 x 768 in bf16: forward with the copy in eight bits 53 us (252 MB, 4.7 TB/s where a copy reaches 5.2), without 40; backward from eight bits onto a residual 70 us
-// (353 MB, 5.0 TB/s), from bf16 77, and 4 us for adding up the blocks' sums in a launch of their own.  2000 x 16384: forward 28 us, backward 77.
+// Bound by memory, 65536 x 768 in bf16: forward with the copy in eight bits 53 us (252 MB, 4.7 TB/s where a copy reaches 5.2), without 41; backward from eight bits onto a residual 70 us
+// (353 MB, 5.0 TB/s), from bf16 77, and 4 us for adding up the blocks' sums in a launch of their own.  2000 x 16384: forward 28.5 us, backward 76.
 #include "cdl_block8.h"
 #include "cdl_chunks.h"
 
@@ -321,7 +321,8 @@ void layer_norm_bwd_kernel(NormBwd a)
 }
 
 constexpr int kForms = 8;
-// lanes of a row, chunks of a lane: up to 128, 256, 512, 1024, 2048, 4096, 8192 and 16384 entries (in 1024 lanes, longer rows would spill: 2000 x 16384 backward 520 us so)
+// lanes of a row, chunks of a lane: up to 128, 256, 512, 1024, 2048, 4096, 8192 and 16384 entries (in 1024 lanes the longest would spill: 2000 x 16384 backward 520 us so.
+// In 512 lanes nothing does where rows are whole; ragged ones keep 4 to 16 registers of a thread in memory, backward: 2000 x 16383 in bf16 91 us where 16384 take 76, in fp32 136 and 123)
 constexpr int kLanes[kForms] = {16, 16, 64, 64, 256, 256, 256, 512}, kChunksOf[kForms] = {1, 2, 1, 2, 1, 2, 4, 4};
 static_assert(kLanes[kForms - 1] * kChunksOf[kForms - 1] * 8 == kNormMostCols, "the longest row");
 int form_of(int32_t cols)

@@ -492,7 +492,7 @@ int cdl_dropout(const void *x, const void *add, int32_t type, int64_t n, float p
  *   weight, bias  fp32[cols], nullable (1 and 0);   y [rows, cols];   mean, rstd  fp32[rows], nullable
  *   q, scale      nullable: x in eight bits for the backward pass, in the same pass over x and byte for byte what cdl_block8_quantize gives
  * What y is off goes with the spread of its row, not with its mean: a row of equal entries is the bias (eps 0: not finite).  The squares are fp32 too: a row of which they pass the largest
- * number has rstd 0.  y may be x.  cols >= 1 unless rows == 0, eps finite and not negative (CDL_ERR_PARAM); CDL_ERR_RANGE for cols > 16384, rows > 2^30 or rows * cols > 2^44.
+ * number has rstd 0, or is not finite where its differences add up to more than that.  y may be x.  cols >= 1 unless rows == 0, eps finite and not negative (CDL_ERR_PARAM); CDL_ERR_RANGE for cols > 16384, rows > 2^30 or rows * cols > 2^44.
  */
 int cdl_layer_norm_fwd(const void *x, int32_t type, const float *weight, const float *bias, int32_t rows, int32_t cols, float eps,
                        void *y, float *mean, float *rstd, uint8_t *q, uint8_t *scale, int32_t format, void *hip_stream);

@@ -1,4 +1,5 @@
-"""What the operators of a feed-forward sublayer promise of their values beyond the roundings' bounds: the same bits whatever else is asked for."""
+"""What the operators of a feed-forward sublayer promise of their values beyond bounds of their roundings: the same bits whatever else is asked for, rows without spread and far from zero,
+what is not finite, products with nothing left out."""
 import pytest
 
 import gpu_util as gu
@@ -140,6 +141,23 @@ def test_a_gradient_alone_is_that_of_a_call_with_sums(env, rows, cols, kind):
         at = su.values(torch, given["q"], given["scale"], cols=cols) if "q" in given else x.double()
         wants = su.norm_back(torch, g.double(), at, w, mean, rstd, add.double(), kind)
         assert torch.equal(*got) and [su.outside(v, *want) for v, want in zip([got[0]] + sums, wants)] == [0, 0, 0]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("cols", [40, 1021, 9000])
+def test_rows_whose_squares_overflow(env, cols, kind):
+    """Squares beyond the largest number of fp32: rstd 0; differences beyond it: not finite; no other row knows of either."""
+    torch, cdl = env
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    x = torch.randn((9, cols), device="cuda", generator=gen).to(getattr(torch, kind))
+    w, b = torch.randn(cols, device="cuda", generator=gen), torch.randn(cols, device="cuda", generator=gen)
+    clean = norm_fwd(torch, cdl, x, w, b)
+    x[2] *= 1e25
+    x[5, ::2], x[5, 1::2] = 3e38, -3e38
+    y, mean, rstd = norm_fwd(torch, cdl, x, w, b)
+    assert float(rstd[2]) == 0 and torch.isfinite(mean[2]) and torch.equal(y[2], b.to(y.dtype)) and not torch.isfinite(y[5]).any()
+    rest = [0, 1, 3, 4, 6, 7, 8]
+    assert all(torch.equal(p[rest], q[rest]) for p, q in zip((y, mean, rstd), clean))
 
 
 # ---- what is not finite ----------------------------------------------------------------------------------------------
